@@ -49,7 +49,20 @@
 extern "C" {
 #endif
 
-enum { XDIT_BF16 = 0, XDIT_F32 = 1 };
+enum { XDIT_BF16 = 0, XDIT_F32 = 1, XDIT_I64 = 2 }; /* XDIT_I64: positions only */
+
+/* Norms of xdit_qk_norm_rope. */
+enum { XDIT_NORM_RMS = 1, XDIT_NORM_LAYER = 2 };
+
+/* Which elements of a head rotate together: neighbours (2i, 2i + 1), or
+ * (i, i + rot_dim / 2). */
+enum { XDIT_PAIRS_INTERLEAVED = 0, XDIT_PAIRS_HALF = 1 };
+
+/* Scaling of a rotary table's frequencies (xdit_rope_table). */
+enum { XDIT_ROPE_NONE = 0, XDIT_ROPE_LINEAR = 1, XDIT_ROPE_NTK = 2, XDIT_ROPE_RAMP = 3 };
+
+/* Upper bound on the axes of one rotary table. */
+#define XDIT_MAX_AXES 4
 
 /* Upper bound on the number of partials one xdit_lse_merge call accepts. */
 #define XDIT_MAX_PARTIALS 64
@@ -305,6 +318,114 @@ int xdit_stage_step(const void* x, const void* wq, const void* wk, const void* w
                     void* kv_buf, int64_t patch_off, int64_t patch_len, void* q, void* k, void* v,
                     void* o, void* y, int64_t batch, int64_t seq_len, int64_t heads,
                     int64_t head_dim, int64_t hidden, int32_t dtype);
+
+/*
+ * The table of a rotary position embedding: of every row, the cosines and
+ * sines of its pairs' angles.  A row has a position on each of n_axes axes
+ * (text, height and width of an image, time of a video); axis a turns
+ * dims[a] / 2 pairs, the axes' pairs one after another:
+ *   angle = position * w,  w = theta^(-2 i / dims[a]),  i = 0 .. dims[a]/2 - 1
+ * Angles are formed and reduced in 64 bits: an angle of size a is off by about
+ * a * 2^-52 before the table is rounded to float32.
+ *   pos      [n, n_axes]  int64 (XDIT_I64) or float32 (XDIT_F32: fractional
+ *                         positions of a grid that is stretched or cropped)
+ *   dims     HOST array of n_axes even positive numbers, at most 256 in all
+ *   scaling  HOST, or NULL for none:
+ *     XDIT_ROPE_LINEAR  w / factor
+ *     XDIT_ROPE_NTK     theta * factor^(dims[a] / (dims[a] - 2)) in theta's
+ *                       place (every dims[a] > 2): the fastest pair keeps its
+ *                       frequency, the slowest is divided by factor
+ *     XDIT_ROPE_RAMP    by the turns that a pair makes over the original
+ *                       length, t = orig_len * w / (2 pi): w where t >= fast,
+ *                       w / factor where t <= slow, linear in t between
+ *                       (fast > slow)
+ *     magnitude         times every cosine and sine, whatever the kind
+ *   cos, sin [n, sum(dims) / 2] float32
+ * n = 0 is a no-op.  cos and sin must not overlap each other or pos.
+ */
+typedef struct {
+    int32_t kind; /* XDIT_ROPE_* */
+    double factor, orig_len, fast, slow, magnitude;
+} xdit_rope_scaling;
+int xdit_rope_table(const void* pos, int32_t pos_dtype, int64_t n, int32_t n_axes, const int32_t* dims,
+                    double theta, const xdit_rope_scaling* scaling, float* cos, float* sin);
+
+/*
+ * Rotation of heads by position: pair (x0, x1) number i of the first rot_dim
+ * elements of each head becomes (x0 c - x1 s, x1 c + x0 s) with c, s of the
+ * row's column i; the other elements are copied.  transpose != 0 turns back
+ * by the same angles: the gradient of the rotation (table magnitudes apply
+ * again, as the gradient has them).
+ *   x, y     [batch, tokens, heads, head_dim]; y may be exactly x (the same
+ *            pointer and strides), must not overlap it otherwise
+ *   strides  HOST array of 2 x 3: the batch, token and head strides of x and
+ *            y in elements (multiples of 16 bytes; the elements of a head are
+ *            contiguous), or NULL for dense tensors
+ *   cos, sin [tokens, rot_dim / 2] float32, or with table_per_batch != 0
+ *            [batch, tokens, rot_dim / 2]; dense, as xdit_rope_table writes them
+ *   rot_dim  a multiple of 8, at most head_dim
+ *   layout   XDIT_PAIRS_*
+ * Products and sums are float32, rounded once.
+ */
+int xdit_rope(const void* x, const float* cos, const float* sin, void* y, const int64_t* strides,
+              int64_t batch, int64_t tokens, int64_t heads, int64_t head_dim, int64_t rot_dim,
+              int32_t table_per_batch, int32_t layout, int32_t transpose, int32_t dtype);
+
+/*
+ * What a layer does to its queries and keys between their projection and the
+ * attention: each head is normalised over its head_dim elements and rotated.
+ *   RMS    n = x / sqrt(mean(x^2) + eps)
+ *   LAYER  n = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps)
+ *   out = rotation(n * w + b)
+ * Queries and keys have weights and biases of their own.  Statistics and
+ * products are float32, rounded once.
+ */
+typedef struct {
+    int64_t batch, tokens, q_heads, k_heads, head_dim; /* k_heads = 0: no keys */
+    int32_t dtype;           /* of queries, keys and their gradients */
+    int32_t norm;            /* XDIT_NORM_* */
+    double eps;
+    const void *wq, *wk;     /* [head_dim], or NULL for ones */
+    const void *bq, *bk;     /* [head_dim], or NULL for zeros; LAYER only */
+    int32_t weight_dtype;    /* of the four: XDIT_BF16 or XDIT_F32 */
+    int32_t layout;          /* XDIT_PAIRS_* */
+    int64_t rot_dim;         /* 0: no rotation (cos and sin NULL) */
+    const float *cos, *sin;  /* as for xdit_rope */
+    int32_t table_per_batch;
+    const int64_t* strides;  /* HOST: batch, token and head strides in elements
+                                of each tensor of the call, in the order of its
+                                arguments, or NULL for dense tensors */
+} xdit_qk;
+
+/*
+ *   q, q_out [batch, tokens, q_heads, head_dim]
+ *   k, k_out [batch, tokens, k_heads, head_dim]
+ * q_out may be exactly q, and k_out exactly k (the same pointer and strides);
+ * otherwise outputs overlap nothing.  Views of one fused projection, whose
+ * rows interleave, count by their heads.  strides: 4 x 3 (q, k, q_out, k_out).
+ */
+int xdit_qk_norm_rope(const xdit_qk* p, const void* q, const void* k, void* q_out, void* k_out);
+
+/*
+ * Gradients of xdit_qk_norm_rope, from its inputs q and k (not kept
+ * normalised) and the gradients of its outputs.
+ *   dq_out, dk_out  gradients of q_out and k_out
+ *   dq, dk          of q and k; dq may be exactly dq_out or q, dk exactly
+ *                   dk_out or k, otherwise they overlap nothing
+ *   dwq, dwk, dbq, dbk  [head_dim] float32 gradients of weights and biases,
+ *                   summed over batch, tokens and heads in float32 in a fixed
+ *                   order; NULL where not wanted (dbq, dbk: LAYER only)
+ *   workspace       xdit_qk_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte
+ *                   aligned, overlapping nothing; unused (may be NULL) when no
+ *                   weight or bias gradient is wanted
+ * strides: 6 x 3 (q, k, dq_out, dk_out, dq, dk).  With no rows the weights'
+ * and biases' gradients are zero.
+ */
+int64_t xdit_qk_norm_rope_bwd_workspace_bytes(int64_t batch, int64_t tokens, int64_t q_heads, int64_t k_heads,
+                                              int64_t head_dim, int32_t dtype);
+int xdit_qk_norm_rope_bwd(const xdit_qk* p, const void* q, const void* k, const void* dq_out,
+                          const void* dk_out, void* dq, void* dk, float* dwq, float* dwk, float* dbq,
+                          float* dbk, void* workspace, int64_t workspace_bytes);
 
 /* Stream for the calling thread's later launches (a hipStream_t; NULL = the
  * default stream).  Always returns XDIT_OK. */

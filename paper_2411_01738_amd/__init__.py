@@ -17,14 +17,15 @@ from __future__ import annotations
 import ctypes
 import warnings
 
-from ._lib import (XDIT_BF16, XDIT_F32, XDIT_MAX_PARTIALS, XDIT_MAX_RANGES, XDIT_MAX_SPLITS,
-                   XditError, check, lib)
+from ._lib import (LAYOUTS, NORMS, SCALINGS, XDIT_BF16, XDIT_F32, XDIT_I64, XDIT_MAX_AXES, XDIT_MAX_PARTIALS,
+                   XDIT_MAX_RANGES, XDIT_MAX_SPLITS, Qk, RopeScaling, XditError, check, lib)
 
 __all__ = ["xdit_patch_attn", "xdit_patch_attn_ranges", "xdit_chunk_attn",
            "xdit_chunk_attn_accum", "xdit_chunk_attn_accum_split", "xdit_chunk_attn_split",
            "xdit_patch_attn_split", "xdit_chunk_attn_split_noalloc",
            "split_workspace_bytes", "xdit_lse_merge",
-           "xdit_kv_update", "xdit_stage_step", "set_stream", "XditError", "XDIT_MAX_PARTIALS", "XDIT_MAX_RANGES",
+           "xdit_kv_update", "xdit_stage_step", "xdit_rope_table", "xdit_rope", "xdit_qk_norm_rope",
+           "xdit_qk_norm_rope_bwd", "qk_norm_rope_bwd_workspace_bytes", "set_stream", "XditError", "XDIT_MAX_PARTIALS", "XDIT_MAX_RANGES",
            "version"]
 
 
@@ -354,3 +355,195 @@ def xdit_stage_step(x, wq, wk, wv, wo, kv_buf, patch_off: int, q, k, v, o, y) ->
     check(lib().xdit_stage_step(_ptr(x), _ptr(wq), _ptr(wk), _ptr(wv), _ptr(wo), _ptr(kv_buf),
                                 int(patch_off), L, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(y), B,
                                 N, H, d, C, _dtype_code(x)))
+
+
+# -- queries and keys between their projection and the attention ----------------
+def _choice(table: dict, what: str, name):
+    code = table.get(name) if isinstance(name, str) else None
+    if code is None:
+        raise XditError(-4, f"{what} = {name!r}, expected one of {', '.join(table)}")
+    return code
+
+
+def _on_device(t, name: str):
+    """A GPU tensor of the current device, whose stream the call goes to."""
+    if not t.is_cuda:
+        raise XditError(-1, f"{name} must be a GPU tensor")
+    if t.device.index != _torch().cuda.current_device():
+        raise XditError(-5, f"{name} is on {t.device}, not on the current device")
+
+
+def _vector(t, name: str, n: int, dtypes):
+    """A dense [n] tensor of one of the types, or None."""
+    if t is None:
+        return
+    _on_device(t, name)
+    if tuple(t.shape) != (n,) or not t.is_contiguous() or t.dtype not in dtypes:
+        raise XditError(-3, f"{name} must be a dense [{n}] tensor of {' or '.join(str(x) for x in dtypes)}")
+
+
+def _head_views(tensors):
+    """Sizes (B, N, d) and strides of [B, N, H, d] tensors whose heads lie
+    contiguous: (tensor, name, shape it must have or None) each; a None tensor
+    has strides 0."""
+    strides = []
+    for t, name, shape, dtype in tensors:
+        if t is None:
+            strides += [0, 0, 0]
+            continue
+        _on_device(t, name)
+        if t.dim() != 4:
+            raise XditError(-3, f"{name} must have 4 dims, got {tuple(t.shape)}")
+        if t.stride(3) != 1:
+            raise XditError(-5, f"{name}: the elements of a head must be contiguous")
+        if tuple(t.shape) != tuple(shape):
+            raise XditError(-3, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.dtype != dtype:
+            raise XditError(-2, f"{name} dtype {t.dtype} differs from {dtype}")
+        strides += t.stride()[:3]
+    return (ctypes.c_int64 * len(strides))(*strides)
+
+
+def _table(cos, sin, B: int, N: int):
+    """(rot_dim, table per batch) of a rotary table, [N, r] or [B, N, r]."""
+    if cos is None and sin is None:
+        return 0, 0
+    torch = _torch()
+    for t, n in ((cos, "cos"), (sin, "sin")):
+        if t is None:
+            raise XditError(-1, "cos and sin go together")
+        _on_device(t, n)
+        if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape[:-1]) not in ((N,), (B, N)):
+            raise XditError(-3, f"{n} must be a dense float32 [{N}, rot / 2] or [{B}, {N}, rot / 2], got {tuple(t.shape)}")
+    if cos.shape != sin.shape:
+        raise XditError(-3, "cos and sin differ in shape")
+    return 2 * cos.shape[-1], int(cos.dim() == 3)
+
+
+def xdit_rope_table(pos, dims, cos, sin, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                    orig_len: float = 0.0, fast: float = 32.0, slow: float = 1.0, magnitude: float = 1.0) -> None:
+    """cos, sin [N, sum(dims) / 2] float32 of the angles of positions pos
+    [N, len(dims)] (int64, or float32 for fractional ones): axis a turns
+    dims[a] / 2 pairs at theta^(-2i / dims[a]).  scaling: "none", "linear" (all
+    frequencies / factor), "ntk" (theta grown so that the slowest pair is
+    divided by factor) or "ramp" (by a pair's turns within orig_len: kept from
+    `fast` turns on, / factor up to `slow`); magnitude multiplies the table."""
+    torch = _torch()
+    dims = [int(x) for x in dims]
+    if not 1 <= len(dims) <= XDIT_MAX_AXES:
+        raise XditError(-4, f"{len(dims)} axes outside [1, {XDIT_MAX_AXES}]")
+    _on_device(pos, "pos")
+    if pos.dtype not in (torch.int64, torch.float32):
+        raise XditError(-2, f"positions are int64 or float32, not {pos.dtype}")
+    if pos.dim() != 2 or pos.shape[1] != len(dims) or not pos.is_contiguous():
+        raise XditError(-3, f"pos must be a dense [N, {len(dims)}] tensor, got {tuple(pos.shape)}")
+    n, cols = pos.shape[0], sum(dims) // 2
+    for t, name in ((cos, "cos"), (sin, "sin")):
+        _on_device(t, name)
+        if t.dtype != torch.float32 or tuple(t.shape) != (n, cols) or not t.is_contiguous():
+            raise XditError(-3, f"{name} must be a dense float32 [{n}, {cols}] tensor")
+    sc = RopeScaling(_choice(SCALINGS, "scaling", scaling), float(factor), float(orig_len), float(fast), float(slow),
+                     float(magnitude))
+    d = (ctypes.c_int32 * len(dims))(*dims)
+    _use_current_stream()
+    check(lib().xdit_rope_table(_ptr(pos), XDIT_I64 if pos.dtype == torch.int64 else XDIT_F32, n, len(dims), d, float(theta),
+                                ctypes.byref(sc), _ptr(cos), _ptr(sin)))
+
+
+def xdit_rope(x, cos, sin, y, layout: str = "interleaved", transpose: bool = False) -> None:
+    """y = x [B, N, H, d] with the first 2 * cos.shape[-1] elements of each head
+    rotated by its row's angles (cos, sin [N, r] or [B, N, r]); pairs of
+    neighbours ("interleaved") or (i, i + r) ("half").  transpose: turned back,
+    the gradient.  x and y may be strided (each head contiguous); y may be x."""
+    nat = _native if _native is not None else _load_native()
+    if nat and _done(nat.rope(x, cos, sin, y, layout, transpose)):
+        return
+    lay = _choice(LAYOUTS, "layout", layout)
+    if x.dim() != 4:
+        raise XditError(-3, f"x must have 4 dims, got {tuple(x.shape)}")
+    code = _dtype_code(x)
+    strides = _head_views([(x, "x", x.shape, x.dtype), (y, "y", x.shape, x.dtype)])
+    B, N, H, d = x.shape
+    if cos is None or sin is None:
+        raise XditError(-1, "cos and sin are required")
+    rot, per_batch = _table(cos, sin, B, N)
+    _use_current_stream()
+    check(lib().xdit_rope(_ptr(x), _ptr(cos), _ptr(sin), _ptr(y), strides, B, N, H, d, rot, per_batch, lay, int(transpose),
+                          code))
+
+
+def _qk(q, k, others, norm, eps, wq, wk, bq, bk, cos, sin, layout):
+    """The parameters of a call on queries and keys; others: (tensor, name,
+    whether of q's shape) in argument order."""
+    torch = _torch()
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise XditError(-3, "q and k must have 4 dims")
+    B, N, H, d = q.shape
+    Hk = 0 if k is None else k.shape[2]
+    code = _dtype_code(q)
+    views = [(q, "q", q.shape, q.dtype), (k, "k", (B, N, Hk, d), q.dtype)]
+    for t, name, as_q in others:
+        if t is None and (as_q or Hk):
+            raise XditError(-1, f"{name} is required")
+        views.append((t, name, (B, N, H if as_q else Hk, d), q.dtype))
+    strides = _head_views(views)
+    weights = [(wq, "wq"), (wk, "wk"), (bq, "bq"), (bk, "bk")]
+    types = {t.dtype for t, _ in weights if t is not None}
+    for t, name in weights:
+        _vector(t, name, d, (torch.bfloat16, torch.float32))
+    if len(types) > 1:
+        raise XditError(-2, "weights and biases of one call have one type")
+    rot, per_batch = _table(cos, sin, B, N)
+    return Qk(B, N, H, Hk, d, code, _choice(NORMS, "norm", norm), float(eps), _ptr(wq), _ptr(wk), _ptr(bq), _ptr(bk),
+              XDIT_BF16 if torch.bfloat16 in types else XDIT_F32, _choice(LAYOUTS, "layout", layout), rot, _ptr(cos),
+              _ptr(sin), per_batch, strides)
+
+
+def xdit_qk_norm_rope(q, k, q_out, k_out, norm: str = "rms", eps: float = 1e-6, wq=None, wk=None, bq=None, bk=None,
+                      cos=None, sin=None, layout: str = "interleaved") -> None:
+    """Queries q [B, N, H, d] and keys k [B, N, Hk, d] (or None) normalised per
+    head ("rms" or "layer", weights [d] and, for "layer", biases [d] of their own,
+    bfloat16 or float32) and rotated as by xdit_rope (no table: not rotated).
+    Tensors may be strided (each head contiguous): views of one fused
+    projection's output; q_out may be q and k_out k."""
+    nat = _native if _native is not None else _load_native()
+    if nat and _done(nat.qk_norm_rope(q, k, q_out, k_out, norm, eps, wq, wk, bq, bk, cos, sin, layout)):
+        return
+    p = _qk(q, k, [(q_out, "q_out", True), (k_out, "k_out", False)], norm, eps, wq, wk, bq, bk, cos, sin, layout)
+    _use_current_stream()
+    check(lib().xdit_qk_norm_rope(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out)))
+
+
+def qk_norm_rope_bwd_workspace_bytes(q, k) -> int:
+    """Bytes of workspace that xdit_qk_norm_rope_bwd needs for the weights'
+    gradients of q [B, N, H, d] and k (or None)."""
+    B, N, H, d = q.shape
+    n = lib().xdit_qk_norm_rope_bwd_workspace_bytes(B, N, H, 0 if k is None else k.shape[2], d, _dtype_code(q))
+    if n < 0:
+        raise XditError(-3, "xdit_qk_norm_rope_bwd_workspace_bytes rejected the sizes")
+    return int(n)
+
+
+def xdit_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, norm: str = "rms", eps: float = 1e-6, wq=None, wk=None, cos=None,
+                          sin=None, layout: str = "interleaved", dwq=None, dwk=None, dbq=None, dbk=None,
+                          workspace=None) -> None:
+    """Gradients of xdit_qk_norm_rope: dq, dk of its inputs q and k, given the
+    gradients dq_out, dk_out of its outputs; and, where given, the float32
+    gradients [d] of weights (dwq, dwk) and, for "layer", biases (dbq, dbk),
+    for which a workspace of qk_norm_rope_bwd_workspace_bytes bytes is needed.
+    dq may be dq_out or q, dk likewise."""
+    nat = _native if _native is not None else _load_native()
+    if nat and _done(nat.qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, norm, eps, wq, wk, cos, sin, layout, dwq, dwk, dbq,
+                                          dbk, workspace)):
+        return
+    torch = _torch()
+    p = _qk(q, k, [(dq_out, "dq_out", True), (dk_out, "dk_out", False), (dq, "dq", True), (dk, "dk", False)], norm, eps, wq,
+            wk, None, None, cos, sin, layout)
+    for t, name in ((dwq, "dwq"), (dwk, "dwk"), (dbq, "dbq"), (dbk, "dbk")):
+        _vector(t, name, q.shape[3], (torch.float32,))
+    if workspace is not None:
+        _on_device(workspace, "workspace")
+    wp, wb = _workspace(workspace)
+    _use_current_stream()
+    check(lib().xdit_qk_norm_rope_bwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk),
+                                      _ptr(dwq), _ptr(dwk), _ptr(dbq), _ptr(dbk), wp, wb))

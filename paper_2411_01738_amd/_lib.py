@@ -19,7 +19,11 @@ STATUS = {
     -4: "XDIT_ERR_RANGE", -5: "XDIT_ERR_LAYOUT", -6: "XDIT_ERR_ALIAS",
     -7: "XDIT_ERR_UNSUPPORTED", -8: "XDIT_ERR_HIP",
 }
-XDIT_BF16, XDIT_F32 = 0, 1
+XDIT_BF16, XDIT_F32, XDIT_I64 = 0, 1, 2
+NORMS = {"rms": 1, "layer": 2}
+LAYOUTS = {"interleaved": 0, "half": 1}
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
+XDIT_MAX_AXES = 4
 XDIT_MAX_PARTIALS = 64
 XDIT_MAX_RANGES = 2
 XDIT_MAX_SPLITS = 16
@@ -27,6 +31,21 @@ XDIT_MAX_SPLITS = 16
 _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _i32 = ctypes.c_int32
+_f64 = ctypes.c_double
+
+
+class RopeScaling(ctypes.Structure):
+    """xdit_rope_scaling"""
+    _fields_ = [("kind", _i32), ("factor", _f64), ("orig_len", _f64), ("fast", _f64), ("slow", _f64), ("magnitude", _f64)]
+
+
+class Qk(ctypes.Structure):
+    """xdit_qk"""
+    _fields_ = [("batch", _i64), ("tokens", _i64), ("q_heads", _i64), ("k_heads", _i64), ("head_dim", _i64),
+                ("dtype", _i32), ("norm", _i32), ("eps", _f64), ("wq", _vp), ("wk", _vp), ("bq", _vp), ("bk", _vp),
+                ("weight_dtype", _i32), ("layout", _i32), ("rot_dim", _i64), ("cos", _vp), ("sin", _vp),
+                ("table_per_batch", _i32), ("strides", ctypes.POINTER(_i64))]
+
 
 SIGNATURES = {
     "xdit_patch_attn": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _i64,
@@ -50,6 +69,12 @@ SIGNATURES = {
     "xdit_kv_update": (ctypes.c_int, [_vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i32]),
     "xdit_stage_step": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp,
                                        _vp, _i64, _i64, _i64, _i64, _i64, _i32]),
+    "xdit_rope_table": (ctypes.c_int, [_vp, _i32, _i64, _i32, _vp, _f64, ctypes.POINTER(RopeScaling), _vp, _vp]),
+    "xdit_rope": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i32, _i32, _i32, _i32]),
+    "xdit_qk_norm_rope": (ctypes.c_int, [ctypes.POINTER(Qk), _vp, _vp, _vp, _vp]),
+    "xdit_qk_norm_rope_bwd_workspace_bytes": (_i64, [_i64, _i64, _i64, _i64, _i64, _i32]),
+    "xdit_qk_norm_rope_bwd": (ctypes.c_int, [ctypes.POINTER(Qk), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                             _i64]),
     "xdit_set_stream": (ctypes.c_int, [_vp]),
     "xdit_get_stream": (_vp, []),
     "xdit_last_error": (ctypes.c_char_p, []),

@@ -242,6 +242,174 @@ PyObject* update(PyObject* const* a) {
     return run([&] { return xdit_kv_update(kv.p, off, len, fk.p, fv.p, B, N, H, d, dt); });
 }
 
+// One [B, N, H, d] tensor argument of any strides whose heads lie contiguous.
+struct V : T {
+    at::IntArrayRef st;
+    c10::DeviceIndex dev = -1;
+};
+
+bool view(PyObject* o, V* t) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor& x = THPVariable_Unpack(o);
+    if (x.layout() != at::kStrided || !x.is_cuda() || x.dim() != 4 || x.stride(3) != 1) return false;
+    t->s = x.sizes();
+    t->st = x.strides();
+    t->dt = x.scalar_type();
+    t->p = x.data_ptr();
+    t->dev = x.device().index();
+    return true;
+}
+
+bool like(const V& t, const V& q, int64_t H) {
+    return t.dev == q.dev && shape4(t, q.dt, q.s[0], q.s[1], H, q.s[3]);
+}
+
+// one of the names, as its place in the list
+template <size_t N>
+bool choice(PyObject* o, const char* const (&names)[N], int32_t first, int32_t* c) {
+    if (!PyUnicode_CheckExact(o)) return false;
+    for (size_t i = 0; i < N; ++i)
+        if (PyUnicode_CompareWithASCIIString(o, names[i]) == 0) {
+            *c = first + (int32_t)i;
+            return true;
+        }
+    return false;
+}
+const char* const kNorms[] = {"rms", "layer"};
+const char* const kLayouts[] = {"interleaved", "half"};
+
+bool device_of(PyObject* o, c10::DeviceIndex dev) { return THPVariable_Unpack(o).device().index() == dev; }
+
+// a dense tensor of the given device, or None
+bool on_device(PyObject* o, int64_t dims, c10::DeviceIndex dev, T* t) {
+    return o == Py_None || (get(o, dims, t) && device_of(o, dev));
+}
+
+// a rotary table of [N, r] or [B, N, r], or none
+bool table(PyObject* co, PyObject* so, const V& x, T* c, T* s, int64_t* rot, int32_t* per_batch) {
+    if (co == Py_None && so == Py_None) {
+        *rot = 0;
+        *per_batch = 0;
+        return true;
+    }
+    if (!get(co, -1, c) || !get(so, -1, s) || !device_of(co, x.dev) || !device_of(so, x.dev) || c->dt != at::kFloat ||
+        s->dt != at::kFloat || c->s != s->s)
+        return false;
+    const size_t n = c->s.size();
+    if (n != 2 && n != 3) return false;
+    if (c->s[n - 2] != x.s[1] || (n == 3 && c->s[0] != x.s[0])) return false;
+    *rot = 2 * c->s[n - 1];
+    *per_batch = n == 3;
+    return true;
+}
+
+// the device whose stream the call goes to
+bool current_device(c10::DeviceIndex* dev) {
+    PyObject* o = PyObject_CallNoArgs(g_device);
+    const long d = o ? PyLong_AsLong(o) : -1;
+    Py_XDECREF(o);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    *dev = (c10::DeviceIndex)d;
+    return true;
+}
+
+// x, cos, sin, y, layout, transpose
+PyObject* rope(PyObject* const* a) {
+    V x, y;
+    T c, s;
+    int64_t rot;
+    int32_t dt, lay, pb;
+    c10::DeviceIndex dev;
+    if (!view(a[0], &x) || !view(a[3], &y) || !like(y, x, x.s[2]) || !code(x.dt, &dt) || a[1] == Py_None ||
+        !table(a[1], a[2], x, &c, &s, &rot, &pb) || !choice(a[4], kLayouts, 0, &lay) || !PyBool_Check(a[5]) ||
+        !current_device(&dev) || dev != x.dev)
+        Py_RETURN_NONE;
+    const int64_t st[6] = {x.st[0], x.st[1], x.st[2], y.st[0], y.st[1], y.st[2]};
+    const int32_t tr = a[5] == Py_True;
+    return run([&] {
+        return xdit_rope(x.p, (const float*)c.p, (const float*)s.p, y.p, st, x.s[0], x.s[1], x.s[2], x.s[3], rot, pb, lay, tr,
+                         dt);
+    });
+}
+
+// The parameters of a call on queries and keys: norm, eps, wq, wk, bq, bk, cos,
+// sin, layout at the given places; bq, bk: nullptr where the call has none.
+bool qk_params(const V& q, const V& k, PyObject* norm, PyObject* eps, PyObject* const (&w)[4], PyObject* co, PyObject* so,
+               PyObject* layout, xdit_qk* p) {
+    T c, s, wt[4];
+    c10::DeviceIndex dev;
+    if (!code(q.dt, &p->dtype) || !choice(norm, kNorms, XDIT_NORM_RMS, &p->norm) || !choice(layout, kLayouts, 0, &p->layout) ||
+        !PyFloat_CheckExact(eps) || !table(co, so, q, &c, &s, &p->rot_dim, &p->table_per_batch) || !current_device(&dev) ||
+        dev != q.dev)
+        return false;
+    p->eps = PyFloat_AS_DOUBLE(eps);
+    p->weight_dtype = -1;
+    for (int i = 0; i < 4; ++i) {
+        if (w[i] == nullptr || w[i] == Py_None) continue;
+        int32_t wc;
+        if (!get(w[i], 1, &wt[i]) || !device_of(w[i], q.dev) || wt[i].s[0] != q.s[3] || !code(wt[i].dt, &wc) ||
+            (p->weight_dtype >= 0 && p->weight_dtype != wc))
+            return false;
+        p->weight_dtype = wc;
+    }
+    if (p->weight_dtype < 0) p->weight_dtype = XDIT_F32;
+    p->batch = q.s[0], p->tokens = q.s[1], p->q_heads = q.s[2], p->head_dim = q.s[3];
+    p->k_heads = k.p == nullptr && k.s.empty() ? 0 : k.s[2];
+    p->wq = wt[0].p, p->wk = wt[1].p, p->bq = wt[2].p, p->bk = wt[3].p;
+    p->cos = (const float*)c.p, p->sin = (const float*)s.p;
+    return true;
+}
+
+// queries' and keys' tensors in argument order; keys' are all None or all given
+template <int N>
+bool qk_views(PyObject* const* a, V (&v)[N], int64_t (&st)[3 * N]) {
+    const bool keys = a[1] != Py_None;
+    for (int i = 0; i < N; ++i) {
+        for (int j = 0; j < 3; ++j) st[3 * i + j] = 0;
+        if (i % 2 == 1 && !keys) {
+            if (a[i] != Py_None) return false;
+            continue;
+        }
+        if (!view(a[i], &v[i]) || !like(v[i], v[0], v[i % 2].s[2])) return false;
+        for (int j = 0; j < 3; ++j) st[3 * i + j] = v[i].st[j];
+    }
+    return true;
+}
+
+// q, k, q_out, k_out, norm, eps, wq, wk, bq, bk, cos, sin, layout
+PyObject* qk_norm_rope(PyObject* const* a) {
+    V v[4];
+    int64_t st[12];
+    xdit_qk p{};
+    PyObject* const w[4] = {a[6], a[7], a[8], a[9]};
+    if (!qk_views(a, v, st) || !qk_params(v[0], v[1], a[4], a[5], w, a[10], a[11], a[12], &p)) Py_RETURN_NONE;
+    p.strides = st;
+    return run([&] { return xdit_qk_norm_rope(&p, v[0].p, v[1].p, v[2].p, v[3].p); });
+}
+
+// q, k, dq_out, dk_out, dq, dk, norm, eps, wq, wk, cos, sin, layout, dwq, dwk, dbq, dbk, workspace
+PyObject* qk_norm_rope_bwd(PyObject* const* a) {
+    V v[6];
+    T g[4], ws;
+    int64_t st[18];
+    xdit_qk p{};
+    PyObject* const w[4] = {a[8], a[9], nullptr, nullptr};
+    if (!qk_views(a, v, st) || !qk_params(v[0], v[1], a[6], a[7], w, a[10], a[11], a[12], &p)) Py_RETURN_NONE;
+    for (int i = 0; i < 4; ++i)
+        if (!on_device(a[13 + i], 1, v[0].dev, &g[i]) ||
+            (a[13 + i] != Py_None && (g[i].dt != at::kFloat || g[i].s[0] != p.head_dim)))
+            Py_RETURN_NONE;
+    if (!on_device(a[17], -1, v[0].dev, &ws)) Py_RETURN_NONE;
+    p.strides = st;
+    return run([&] {
+        return xdit_qk_norm_rope_bwd(&p, v[0].p, v[1].p, v[2].p, v[3].p, v[4].p, v[5].p, (float*)g[0].p, (float*)g[1].p,
+                                     (float*)g[2].p, (float*)g[3].p, ws.p, ws.bytes);
+    });
+}
+
 // device, raw_stream: the callables that give torch's current stream
 PyObject* init(PyObject* const* a) {
     Py_INCREF(a[0]);
@@ -254,7 +422,8 @@ PyObject* init(PyObject* const* a) {
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))&entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(init, 2),         ENTRY(chunk, 6),       ENTRY(chunk_split, 8),
                          ENTRY(patch, 7),        ENTRY(patch_ranges, 7), ENTRY(patch_split, 9),
-                         ENTRY(merge, 5),        ENTRY(update, 5),      {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(merge, 5),        ENTRY(update, 5),      ENTRY(rope, 6),
+                         ENTRY(qk_norm_rope, 13), ENTRY(qk_norm_rope_bwd, 18), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

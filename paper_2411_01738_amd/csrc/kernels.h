@@ -57,6 +57,49 @@ struct UpdateParams {
     int esize;                // bytes per element
 };
 
+// Rows of one head, [B, N, H, D] with the strides (in elements) of any order.
+struct HeadView {
+    const void* p;
+    int64_t sb, st, sh;  // batch, token, head
+};
+
+// Queries (side 0) and keys (side 1) normalised per head and rotated, or the
+// gradients of that.  A side with no heads is absent.
+struct NormRopeSide {
+    HeadView x, g, y;    // input; gradient of the output (backward); output, or the input's gradient
+    const void* w;       // [D] weight and bias, or nullptr
+    const void* b;
+    float* dw;           // [D] gradients of weight and bias, or nullptr
+    float* db;
+    int heads;
+};
+
+struct NormRopeParams {
+    NormRopeSide side[2];
+    const float* cos;    // [N, rot / 2] (table_batch = 0) or [B, N, rot / 2]
+    const float* sin;
+    int64_t table_batch; // elements between the tables of two batches
+    int B, N, D, rot;
+    int bf16, weight_bf16;
+    int norm;            // XDIT_NORM_*
+    int half;            // pairs (i, i + rot / 2) instead of (2i, 2i + 1)
+    int transpose;       // rotate by the negative angles (no norm)
+    float eps;
+    float* part;         // backward: workspace of norm_rope_bwd_partials
+};
+
+struct RopeTableParams {
+    const void* pos;     // [n, axes], int64 or float32
+    int pos_i64;
+    int axes;
+    int dims[4];         // rotated dims of each axis, even
+    double theta, factor, orig_len, fast, slow, magnitude;
+    int scaling;         // XDIT_ROPE_*
+    float* cos;          // [n, sum(dims) / 2]
+    float* sin;
+    int64_t n;
+};
+
 constexpr int kMaxPartials = 64;
 constexpr int kPartSlotRows = 128;  // query rows of a partitioned launch's tile
 constexpr int kMaxSweepParts = 17;  // most partition ranges one sweep may meet
@@ -80,5 +123,12 @@ hipError_t launch_attn_f32(const AttnParams& p, hipStream_t s);
 hipError_t launch_merge_bf16(const MergeParams& p, hipStream_t s);
 hipError_t launch_merge_f32(const MergeParams& p, hipStream_t s);
 hipError_t launch_kv_update(const UpdateParams& p, hipStream_t s);
+hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t s);
+// The gradients of the norm and rotation: dx per head (side[].y), and the
+// weights' and biases' gradients by way of p.part
+// (norm_rope_bwd_partials floats).
+hipError_t launch_norm_rope_bwd(const NormRopeParams& p, hipStream_t s);
+int64_t norm_rope_bwd_partials(int64_t rows, int heads0, int heads1, int D, bool bf16);
+hipError_t launch_rope_table(const RopeTableParams& p, hipStream_t s);
 
 }  // namespace xdit

@@ -1,0 +1,489 @@
+// What a layer does to its queries and keys between their projection and the
+// attention: a norm over each head's D values and the rotation of pairs of
+// them by the token's position, in one pass, and the gradients of both; the
+// rotation alone; and the table of the angles' cosines and sines.
+//
+// Per head x of D values, with weight w and bias b (or none):
+//   rms    n = x r,             r = 1 / sqrt(mean(x^2) + eps)
+//   layer  n = (x - mean(x)) r, r = 1 / sqrt(mean((x - mean(x))^2) + eps)
+//   y = R (n w + b), R rotating pair i of the first `rot` dims by angle i:
+//   y0 = x0 c - x1 s, y1 = x1 c + x0 s, pairs (2i, 2i + 1) or (i, i + rot/2).
+// Backward, with g the gradient of y and h = R^T g (the same rotation with -s):
+//   db = sum h, dw = sum h n over all rows,
+//   dx = r (h w - n mean(h w n) [- mean(h w) for the layer norm]).
+// All of it in float32, rounded once at the store.
+//
+// What bounds it: memory.  Each head is read and written once; the tables are
+// read once per token and batch of heads.
+//
+// Work: a lane holds 2 V values of a head, both elements of each of its
+// pairs, so the rotation needs no other lane: the runs [2 V p, 2 V p + 2 V) for
+// neighbouring pairs, the runs at V p and rot / 2 + V p for pairs half a
+// rotation apart.  D / (2 V) lanes hold a head and share its sums; a wave
+// holds 64 / that many heads (7 at D = 72, one lane idle) and walks over
+// tokens with the same heads, so weights stay in registers and the angles of a
+// token are loaded once for up to kBatch heads of a lane.
+#include "kernels.h"
+
+#include <math.h>
+
+namespace xdit {
+namespace {
+
+#include "attn_common.h"
+
+constexpr int kWaves = 4;   // waves per workgroup, a token each at a time
+constexpr int kBatch = 4;   // heads of a lane per token, their loads issued together
+
+struct NrSide {
+    const char* x;
+    const char* g;
+    char* y;
+    int64_t xb, xt, xh, gb, gt, gh, yb, yt, yh;  // byte strides
+    const void* w;
+    const void* b;
+    int heads;
+    int grads;  // bit 0: weight, bit 1: bias
+};
+
+struct NrArgs {
+    NrSide side[2];
+    int nb0;  // batches of heads of side 0 (blockIdx.y below it)
+    const float* cos;
+    const float* sin;
+    int64_t table_batch;
+    uint32_t rows, N;
+    int rot, half, weight_bf16;
+    float sgn, eps;
+    float* part;       // partials of side 0: weight's, then bias's; then side 1's
+    int64_t part1;     // first partial (in floats) of side 1
+};
+
+__device__ __forceinline__ float bf16f(uint32_t lo16) { return __uint_as_float(lo16 << 16); }
+
+// A run of V values of type T as it lies in memory, and to float32
+template <typename T, int V>
+struct Run;
+template <>
+struct Run<uint16_t, 8> {
+    typedef u32x4 Raw;
+};
+template <>
+struct Run<uint16_t, 4> {
+    typedef u32x2 Raw;
+};
+template <>
+struct Run<float, 4> {
+    typedef f32x4 Raw;
+};
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const typename Run<T, V>::Raw& r, float* f) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = r[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) {
+            f[2 * e] = bf16f(r[e] & 0xffffu);
+            f[2 * e + 1] = __uint_as_float(r[e] & 0xffff0000u);
+        }
+    }
+}
+// float32 values rounded to nearest even and stored
+template <typename T, int V>
+__device__ __forceinline__ void store_run(char* p, const float* f) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) *(f32x4*)(p + 4 * i) = f32x4{f[i], f[i + 1], f[i + 2], f[i + 3]};
+    } else if constexpr (V == 8) {
+        *(u32x4*)p = u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                           pack_bf16x2(f[6], f[7])};
+    } else {
+        *(u32x2*)p = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+    }
+}
+// V weights from element e on, of either type; `fill` where there are none
+template <int V>
+__device__ __forceinline__ void load_weights(const void* w, int is_bf16, int e, float fill, float* f) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        f[i] = w == nullptr ? fill : is_bf16 ? bf16f(((const uint16_t*)w)[e + i]) : ((const float*)w)[e + i];
+}
+
+// Sum over the L lanes of a head, the same bits in each of them.
+template <int L>
+__device__ __forceinline__ float head_sum(float v, int lane, int p) {
+    if constexpr (L == 9) {  // by threes
+        const int t = lane - p % 3;
+        v = __shfl(v, t) + __shfl(v, t + 1) + __shfl(v, t + 2);
+        const int h = lane - p;
+        return __shfl(v, h) + __shfl(v, h + 3) + __shfl(v, h + 6);
+    } else {
+#pragma unroll
+        for (int o = 1; o < L; o *= 2) v += __shfl_xor(v, o);
+        return v;
+    }
+}
+
+// The first `turning` pairs of a lane's values rotated by (c, s): pairs of
+// neighbours, or of the runs a and b = a + V.  The others stay as they are,
+// whatever stands beside them.
+template <int V>
+__device__ __forceinline__ void rotate(float* x, const float* c, const float* s, int turning, bool half) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float a = half ? x[i] : x[2 * i], b = half ? x[V + i] : x[2 * i + 1];
+        const bool on = i < turning;
+        const float ya = on ? a * c[i] - b * s[i] : a, yb = on ? b * c[i] + a * s[i] : b;
+        if (half) {
+            x[i] = ya;
+            x[V + i] = yb;
+        } else {
+            x[2 * i] = ya;
+            x[2 * i + 1] = yb;
+        }
+    }
+}
+
+template <typename T, int D, int V, int NORM, bool BWD, bool HALF>
+__global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
+    constexpr int L = D / (2 * V), G = 64 / L, ES = sizeof(T);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int p = lane % L, grp = lane / L;
+    const bool second = (int)blockIdx.y >= a.nb0;
+    const NrSide& sd = a.side[second];
+    const int head0 = ((int)blockIdx.y - (second ? a.nb0 : 0)) * kBatch * G + grp;
+    const int rp = a.rot / 2;
+
+    // this lane's two runs of V elements, and the pair that the first belongs to
+    const int col = V * p;
+    int oa = 2 * V * p, ob = oa + V;
+    if (HALF) {
+        if (col < rp) oa = col, ob = rp + col;
+        else oa = a.rot + 2 * (col - rp), ob = oa + V;
+    }
+    const int turning = rp - col;  // pairs of this lane that rotate (a multiple of 4, or none)
+    float w[2 * V], bias[2 * V];
+    if constexpr (NORM != 0) {
+        load_weights<V>(sd.w, a.weight_bf16, oa, 1.f, w);
+        load_weights<V>(sd.w, a.weight_bf16, ob, 1.f, w + V);
+        if constexpr (!BWD) {
+            load_weights<V>(sd.b, a.weight_bf16, oa, 0.f, bias);
+            load_weights<V>(sd.b, a.weight_bf16, ob, 0.f, bias + V);
+        }
+    }
+    float dw[2 * V], db[2 * V];
+    if constexpr (BWD)
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) dw[i] = db[i] = 0.f;
+
+    for (uint32_t row = blockIdx.x * kWaves + wave; row < a.rows; row += gridDim.x * kWaves) {
+        const uint32_t b = row / a.N, n = row - b * a.N;
+        float c[V], s[V];
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            f32x4 cv = {}, sv = {};
+            if (i < turning) {
+                const int64_t at = b * a.table_batch + (int64_t)n * rp + col + i;
+                cv = *(const f32x4*)(a.cos + at);
+                sv = *(const f32x4*)(a.sin + at) * a.sgn;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[i + e] = cv[e], s[i + e] = sv[e];
+        }
+        // the loads of a lane's heads together, as they lie in memory
+        typedef typename Run<T, V>::Raw Raw;
+        Raw x[kBatch][2], g[BWD ? kBatch : 1][2];
+        const char* px = sd.x + b * sd.xb + n * sd.xt;
+        const char* pg = BWD ? sd.g + b * sd.gb + n * sd.gt : nullptr;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int h = head0 + u * G;
+            x[u][0] = x[u][1] = Raw{};
+            if constexpr (BWD) g[u][0] = g[u][1] = Raw{};
+            if (grp < G && h < sd.heads) {
+                x[u][0] = *(const Raw*)(px + h * sd.xh + ES * oa);
+                x[u][1] = *(const Raw*)(px + h * sd.xh + ES * ob);
+                if constexpr (BWD) {
+                    g[u][0] = *(const Raw*)(pg + h * sd.gh + ES * oa);
+                    g[u][1] = *(const Raw*)(pg + h * sd.gh + ES * ob);
+                }
+            }
+        }
+        char* py = sd.y + b * sd.yb + n * sd.yt;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int h = head0 + u * G;
+            const bool live = grp < G && h < sd.heads;
+            if (head0 - grp + u * G >= sd.heads) break;  // no head of the wave is left
+            float v[2 * V];
+            unpack<T, V>(x[u][0], v);
+            unpack<T, V>(x[u][1], v + V);
+            if constexpr (NORM == 2) {
+                float m = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) m += v[i];
+                m = head_sum<L>(m, lane, p) * (1.f / D);
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) v[i] -= m;
+            }
+            if constexpr (NORM != 0) {
+                float q = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) q = __builtin_fmaf(v[i], v[i], q);
+                q = head_sum<L>(q, lane, p);
+                // lanes without a head hold zeros: no quotient of theirs reaches a sum
+                const float r = live ? 1.f / __builtin_sqrtf(q * (1.f / D) + a.eps) : 0.f;
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) v[i] *= r;
+                if constexpr (!BWD) {
+#pragma unroll
+                    for (int i = 0; i < 2 * V; ++i) v[i] = __builtin_fmaf(v[i], w[i], bias[i]);
+                } else {
+                    float gv[2 * V];
+                    unpack<T, V>(g[u][0], gv);
+                    unpack<T, V>(g[u][1], gv + V);
+                    rotate<V>(gv, c, s, turning, HALF);
+                    float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 2 * V; ++i) {
+                        dw[i] = __builtin_fmaf(gv[i], v[i], dw[i]);
+                        if constexpr (NORM == 2) db[i] += gv[i];
+                        gv[i] *= w[i];
+                        m1 = __builtin_fmaf(gv[i], v[i], m1);
+                        if constexpr (NORM == 2) m2 += gv[i];
+                    }
+                    m1 = head_sum<L>(m1, lane, p) * (1.f / D);
+                    if constexpr (NORM == 2) m2 = head_sum<L>(m2, lane, p) * (1.f / D);
+#pragma unroll
+                    for (int i = 0; i < 2 * V; ++i) v[i] = r * (gv[i] - __builtin_fmaf(v[i], m1, m2));
+                }
+            }
+            if constexpr (!BWD) rotate<V>(v, c, s, turning, HALF);
+            if (live) {
+                store_run<T, V>(py + h * sd.yh + ES * oa, v);
+                store_run<T, V>(py + h * sd.yh + ES * ob, v + V);
+            }
+        }
+    }
+
+    // the workgroup's sums of the weights' gradients, heads and waves in order
+    if constexpr (BWD) {
+        __shared__ float red[64 * kWaves * 2 * V];
+        const int64_t slots = (int64_t)gridDim.x * (second ? gridDim.y - a.nb0 : a.nb0);
+        const int64_t slot = (int64_t)(blockIdx.y - (second ? a.nb0 : 0)) * gridDim.x + blockIdx.x;
+#pragma unroll
+        for (int k = 0; k < (NORM == 2 ? 2 : 1); ++k) {
+            if (!(sd.grads & (1 << k))) continue;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) red[threadIdx.x * 2 * V + i] = k == 0 ? dw[i] : db[i];
+            __syncthreads();
+            if (threadIdx.x < D) {
+                const int tp = threadIdx.x / (2 * V), ti = threadIdx.x % (2 * V);
+                float sum = 0.f;
+                for (int j = 0; j < kWaves * G; ++j)
+                    sum += red[((j / G) * 64 + (j % G) * L + tp) * 2 * V + ti];
+                int e = 2 * V * tp + ti;
+                if (HALF) {
+                    const int tc = V * tp;
+                    if (tc < rp) e = (ti < V ? tc : rp + tc - V) + ti;
+                    else e = a.rot + 2 * (tc - rp) + ti;
+                }
+                a.part[(second ? a.part1 : 0) + (k * slots + slot) * D + e] = sum;
+            }
+        }
+    }
+}
+
+// Sums of the partials, one output column per 16 threads' rows, in a fixed
+// order.  blockIdx.y: weight and bias of side 0, then of side 1.
+struct NrSumArgs {
+    const float* part[4];
+    float* out[4];
+    int slots[4];
+    int D;
+};
+constexpr int kSumCols = 16, kSumRows = 16;
+
+__global__ __launch_bounds__(kSumCols* kSumRows) void norm_rope_sum_kernel(NrSumArgs a) {
+    __shared__ float red[kSumRows][kSumCols + 1];
+    const int tx = threadIdx.x % kSumCols, ty = threadIdx.x / kSumCols;
+    const int q = blockIdx.y, e = blockIdx.x * kSumCols + tx;
+    if (a.out[q] == nullptr) return;
+    float sum = 0.f;
+    if (e < a.D)
+        for (int j = ty; j < a.slots[q]; j += kSumRows) sum += a.part[q][(int64_t)j * a.D + e];
+    red[ty][tx] = sum;
+    __syncthreads();
+    if (ty == 0 && e < a.D) {
+        for (int j = 1; j < kSumRows; ++j) sum += red[j][tx];
+        a.out[q][e] = sum;
+    }
+}
+
+struct NrGrid {
+    int nb0, nb1;
+    unsigned gx;
+};
+
+// Workgroups along the tokens: one token per wave, and no more waves than the
+// chip holds at once, so that a wave's weights serve several tokens.
+NrGrid nr_grid(int64_t rows, int heads0, int heads1, int G, bool bwd) {
+    NrGrid r;
+    r.nb0 = (heads0 + kBatch * G - 1) / (kBatch * G);
+    r.nb1 = (heads1 + kBatch * G - 1) / (kBatch * G);
+    const int64_t need = (rows + kWaves - 1) / kWaves, nb = r.nb0 + r.nb1 > 0 ? r.nb0 + r.nb1 : 1;
+    const int64_t most = (bwd ? 1024 : 2048) / nb > 1 ? (bwd ? 1024 : 2048) / nb : 1;
+    r.gx = (unsigned)(need < most ? need : most);
+    return r;
+}
+
+// values of a run: 16 bytes where a head's lanes divide it so, 4 values otherwise
+int run_of(int D, bool bf16, int rot, int half) {
+    return bf16 && D % 16 == 0 && (!half || rot % 16 == 0) ? 8 : 4;
+}
+
+template <typename T, int D, int V>
+hipError_t launch_form(const NrArgs& a, dim3 grid, int norm, int half, bool bwd, hipStream_t s) {
+    const dim3 block(64 * kWaves);
+#define XDIT_NR(N, W, F) hipLaunchKernelGGL((norm_rope_kernel<T, D, V, N, W, F>), grid, block, 0, s, a)
+    if (bwd) {
+        if (norm == 1) {
+            if (half) XDIT_NR(1, true, true);
+            else XDIT_NR(1, true, false);
+        } else {
+            if (half) XDIT_NR(2, true, true);
+            else XDIT_NR(2, true, false);
+        }
+    } else if (norm == 0) {
+        if (half) XDIT_NR(0, false, true);
+        else XDIT_NR(0, false, false);
+    } else if (norm == 1) {
+        if (half) XDIT_NR(1, false, true);
+        else XDIT_NR(1, false, false);
+    } else {
+        if (half) XDIT_NR(2, false, true);
+        else XDIT_NR(2, false, false);
+    }
+#undef XDIT_NR
+    return hipGetLastError();
+}
+
+hipError_t launch_any(const NormRopeParams& p, bool bwd, hipStream_t s) {
+    const int V = run_of(p.D, p.bf16, p.rot, p.half);
+    const int64_t es = p.bf16 ? 2 : 4;
+    const int64_t rows = (int64_t)p.B * p.N;
+    const NrGrid g = nr_grid(rows, p.side[0].heads, p.side[1].heads, 64 / (p.D / (2 * V)), bwd);
+    const dim3 grid(g.gx, (unsigned)(g.nb0 + g.nb1));
+    NrArgs a{};
+    for (int i = 0; i < 2; ++i) {
+        const NormRopeSide& f = p.side[i];
+        NrSide& t = a.side[i];
+        t.x = (const char*)f.x.p, t.xb = es * f.x.sb, t.xt = es * f.x.st, t.xh = es * f.x.sh;
+        t.g = (const char*)f.g.p, t.gb = es * f.g.sb, t.gt = es * f.g.st, t.gh = es * f.g.sh;
+        t.y = (char*)f.y.p, t.yb = es * f.y.sb, t.yt = es * f.y.st, t.yh = es * f.y.sh;
+        t.w = f.w, t.b = f.b, t.heads = f.heads;
+        t.grads = (f.dw ? 1 : 0) | (f.db ? 2 : 0);
+    }
+    a.nb0 = g.nb0;
+    a.cos = p.cos, a.sin = p.sin, a.table_batch = p.table_batch;
+    a.rows = (uint32_t)rows, a.N = (uint32_t)(p.N > 0 ? p.N : 1);
+    a.rot = p.cos ? p.rot : 0, a.half = p.half, a.weight_bf16 = p.weight_bf16;
+    a.sgn = bwd || p.transpose ? -1.f : 1.f;
+    a.eps = p.eps;
+    a.part = p.part;
+    a.part1 = (int64_t)2 * g.nb0 * g.gx * p.D;
+    const int half = p.half && a.rot > 0;
+    if (grid.x > 0 && grid.y > 0) {
+        hipError_t e = hipErrorInvalidValue;
+        if (p.bf16) {
+            if (p.D == 64) e = V == 8 ? launch_form<uint16_t, 64, 8>(a, grid, p.norm, half, bwd, s)
+                                      : launch_form<uint16_t, 64, 4>(a, grid, p.norm, half, bwd, s);
+            else if (p.D == 72) e = launch_form<uint16_t, 72, 4>(a, grid, p.norm, half, bwd, s);
+            else if (p.D == 128) e = V == 8 ? launch_form<uint16_t, 128, 8>(a, grid, p.norm, half, bwd, s)
+                                            : launch_form<uint16_t, 128, 4>(a, grid, p.norm, half, bwd, s);
+        } else {
+            if (p.D == 64) e = launch_form<float, 64, 4>(a, grid, p.norm, half, bwd, s);
+            else if (p.D == 72) e = launch_form<float, 72, 4>(a, grid, p.norm, half, bwd, s);
+            else if (p.D == 128) e = launch_form<float, 128, 4>(a, grid, p.norm, half, bwd, s);
+        }
+        if (e != hipSuccess) return e;
+    }
+    if (!bwd) return hipSuccess;
+    NrSumArgs r{};
+    r.D = p.D;
+    bool any = false;
+    for (int i = 0; i < 2; ++i) {
+        const int nb = i == 0 ? g.nb0 : g.nb1;
+        float* out[2] = {p.side[i].dw, p.side[i].db};
+        for (int k = 0; k < 2; ++k) {
+            r.out[2 * i + k] = out[k];
+            r.slots[2 * i + k] = (int)(nb * g.gx);
+            r.part[2 * i + k] = a.part + (i ? a.part1 : 0) + (int64_t)k * nb * g.gx * p.D;
+            any = any || out[k] != nullptr;
+        }
+    }
+    if (!any) return hipSuccess;
+    hipLaunchKernelGGL(norm_rope_sum_kernel, dim3((p.D + kSumCols - 1) / kSumCols, 4), dim3(kSumCols * kSumRows), 0, s, r);
+    return hipGetLastError();
+}
+
+// One thread per column and run of rows: its frequency once, in 64 bits (an
+// angle of 10^6 in float32 is off by 0.06), then per row the product with
+// the position, reduced to a turn and handed to sincospi.
+__global__ __launch_bounds__(256) void rope_table_kernel(RopeTableParams a, int cols, int rows_per_block) {
+    const int col = threadIdx.x % cols, sub = threadIdx.x / cols;
+    if (sub >= rows_per_block) return;
+    int axis = 0, i = col;
+    while (axis + 1 < a.axes && i >= a.dims[axis] / 2) i -= a.dims[axis++] / 2;
+    const double dim = a.dims[axis];
+    double theta = a.theta;
+    if (a.scaling == 2) theta *= pow(a.factor, dim / (dim - 2.0));
+    double w = pow(theta, -2.0 * i / dim);
+    constexpr double kTurn = 0.15915494309189533577;  // 1 / (2 pi)
+    if (a.scaling == 1) w /= a.factor;
+    if (a.scaling == 3) {
+        const double share = fmin(1.0, fmax(0.0, (a.orig_len * w * kTurn - a.slow) / (a.fast - a.slow)));
+        w = w * (share + (1.0 - share) / a.factor);
+    }
+    for (int64_t n = (int64_t)blockIdx.x * rows_per_block + sub; n < a.n; n += (int64_t)gridDim.x * rows_per_block) {
+        const double pos = a.pos_i64 ? (double)((const int64_t*)a.pos)[n * a.axes + axis]
+                                     : (double)((const float*)a.pos)[n * a.axes + axis];
+        const double t = pos * w * kTurn;
+        double sn, cs;
+        sincospi(2.0 * (t - rint(t)), &sn, &cs);
+        a.cos[n * cols + col] = (float)(cs * a.magnitude);
+        a.sin[n * cols + col] = (float)(sn * a.magnitude);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t s) { return launch_any(p, false, s); }
+hipError_t launch_norm_rope_bwd(const NormRopeParams& p, hipStream_t s) { return launch_any(p, true, s); }
+
+int64_t norm_rope_bwd_partials(int64_t rows, int heads0, int heads1, int D, bool bf16) {
+    // either width of a run may be the one that the call's rotation needs
+    int64_t most = 0;
+    for (int V : {4, 8}) {
+        if (V == 8 && run_of(D, bf16, 0, 0) != 8) continue;
+        const NrGrid g = nr_grid(rows, heads0, heads1, 64 / (D / (2 * V)), true);
+        const int64_t n = (int64_t)2 * (g.nb0 + g.nb1) * g.gx * D;
+        if (n > most) most = n;
+    }
+    return most;
+}
+
+hipError_t launch_rope_table(const RopeTableParams& p, hipStream_t s) {
+    int cols = 0;
+    for (int i = 0; i < p.axes; ++i) cols += p.dims[i] / 2;
+    const int rpb = 256 / cols;
+    int64_t blocks = (p.n + rpb - 1) / rpb;
+    if (blocks == 0) return hipSuccess;
+    if (blocks > 2048) blocks = 2048;
+    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(256), 0, s, p, cols, rpb);
+    return hipGetLastError();
+}
+
+}  // namespace xdit

@@ -1,0 +1,401 @@
+"""Rotary tables, rotation, and the norms of queries and keys with it, against
+the formulas in 64 bits.
+
+Error bounds: every result is formed in float32 from terms that `scale` bounds
+(tests/layer_ref.py) and rounded once.  Between them stand at most 64 roundings
+of half a float32 step (a head's sum has 16 terms in a lane and 4 levels
+across lanes; then the mean, eps, root, quotient, weight, bias and the
+rotation's three), so |error| <= 64 * 2^-24 * scale, plus half a step of the
+result's type.  A weight's gradient is a sum over rows: at most 256 additions
+one after another (tokens of a wave, heads, waves, workgroups) of terms with
+that error, so 320 * 2^-24 times the sum of the absolute terms."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import paper_2411_01738_amd as xd
+from tests import layer_ref as ref
+from tests.gpu_util import tdtype, to_np, torch_mod
+
+pytestmark = pytest.mark.gpu
+
+
+def _close(got, want, scale, dtype, what, steps=64):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert got.shape == want.shape, f"{what}: {got.shape} for {want.shape}"
+    bound = ref.HALF[dtype] * np.abs(want) + (1 + ref.HALF[dtype]) * steps * ref.F32 * scale
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, worst {np.nanmax(np.abs(got - want) - bound):.3e} over"
+
+
+class Draws:
+    def __init__(self, seed):
+        self.torch = torch_mod()
+        self.g = self.torch.Generator().manual_seed(seed)
+
+    def __call__(self, *shape, dtype="bf16", scale=1.0, shift=0.0):
+        x = self.torch.randn(*shape, generator=self.g, dtype=self.torch.float32) * scale + shift
+        return x.to(tdtype(dtype)).cuda()
+
+    def angles(self, *shape):
+        a = self.torch.rand(*shape, generator=self.g, dtype=self.torch.float64) * 1000
+        return a.cos().float().cuda(), a.sin().float().cuda()
+
+
+def _np(t):
+    return None if t is None else to_np(t).astype(np.float64)
+
+
+def _np32(t):
+    return None if t is None else t.cpu().numpy().astype(np.float64)
+
+
+# -- tables -------------------------------------------------------------------
+@pytest.mark.parametrize("n,dims,kw", [
+    (1, [128], {}), (77, [16, 56, 56], {}), (300, [16, 24, 24], dict(theta=256.0, magnitude=1.2)), (513, [72], {}),
+    (130, [64], dict(scaling="linear", factor=4.0)), (130, [40, 24], dict(scaling="ntk", factor=2.5)),
+    (130, [128], dict(scaling="ramp", factor=8.0, orig_len=4096, magnitude=1.1, theta=500000.0)),
+    (65, [64], dict(scaling="ramp", factor=3.0, orig_len=100, fast=4.0, slow=0.5)), (9, [2, 2, 4, 2], {}), (5, [256], {})])
+@pytest.mark.parametrize("kind", ["int64", "float32", "far"])
+def test_table(n, dims, kw, kind):
+    torch = torch_mod()
+    g = torch.Generator().manual_seed(n)
+    if kind == "float32":
+        pos = torch.rand(n, len(dims), generator=g) * 300 - 20
+    else:
+        pos = torch.randint(0, 5000, (n, len(dims)), generator=g) + (1 << 24 if kind == "far" else -100)
+    cos, sin = (torch.full((n, sum(dims) // 2), float("nan"), device="cuda") for _ in range(2))
+    xd.xdit_rope_table(pos.cuda(), dims, cos, sin, **kw)
+    c, s = ref.table(pos.numpy(), dims, **kw)
+    # half a float32 step; the angle's own error, 4 roundings of 64 bits
+    ang = 8 * 2.0 ** -53 * float(pos.abs().max()) * kw.get("magnitude", 1.0)
+    for got, want, what in ((cos, c, "cos"), (sin, s, "sin")):
+        err = np.abs(got.cpu().numpy().astype(np.float64) - want)
+        assert (err <= 2.0 ** -24 * np.abs(want) + ang + 1e-12).all(), f"{what}: {err.max():.3e}"
+
+
+def test_table_of_no_rows():
+    torch = torch_mod()
+    e = torch.empty(0, 32, device="cuda")
+    xd.xdit_rope_table(torch.empty(0, 1, device="cuda", dtype=torch.int64), [64], e, e.clone())
+
+
+# -- rotation -----------------------------------------------------------------
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rot", [(64, 64), (64, 40), (64, 8), (72, 72), (72, 24), (128, 128), (128, 56), (128, 64)])
+def test_rope(d, rot, dtype, layout):
+    torch = torch_mod()
+    r = Draws(d + rot)
+    for (B, N, H), per_batch, transpose in [((2, 37, 3), False, False), ((1, 1, 24), False, True), ((2, 130, 17), True, True),
+                                            ((3, 5, 1), True, False)]:
+        x = r(B, N, H, d, dtype=dtype)
+        cos, sin = r.angles(*((B, N) if per_batch else (N,)), rot // 2)
+        y = torch.full_like(x, float("nan"))
+        xd.xdit_rope(x, cos, sin, y, layout=layout, transpose=transpose)
+        want = ref.rotate(_np(x), _np32(cos), _np32(sin), layout, transpose)
+        _close(_np(y), want, 2 * np.abs(_np(x)).max(-1, keepdims=True), dtype, f"{B}x{N}x{H}", steps=3)
+        assert torch.equal(y[..., rot:], x[..., rot:])
+        keep = x.clone()
+        xd.xdit_rope(keep, cos, sin, keep, layout=layout, transpose=transpose)  # in place
+        assert torch.equal(keep, y)
+
+
+def test_rope_leaves_the_other_dims_alone():
+    """Whatever stands in them, and beside them in a lane."""
+    torch = torch_mod()
+    r = Draws(7)
+    for d, rot, layout in [(64, 40, "interleaved"), (64, 40, "half"), (128, 64, "half"), (72, 8, "interleaved")]:
+        x = r(1, 9, 5, d)
+        cos, sin = r.angles(9, rot // 2)
+        want = torch.empty_like(x)
+        xd.xdit_rope(x, cos, sin, want, layout=layout)
+        x[..., rot::3] = float("inf")
+        x[..., rot + 1::3] = float("nan")
+        y = torch.empty_like(x)
+        xd.xdit_rope(x, cos, sin, y, layout=layout)
+        assert torch.equal(y[..., :rot], want[..., :rot])
+        assert torch.equal(y[..., rot:].view(torch.int16), x[..., rot:].view(torch.int16))
+
+
+def test_rope_strided():
+    """Head-major tensors, rows of a longer buffer, every other token."""
+    torch = torch_mod()
+    r = Draws(8)
+    B, N, H, d = 2, 21, 6, 64
+    cos, sin = r.angles(N, d // 2)
+    for x in (r(B, H, N, d).transpose(1, 2), r(B, N + 9, H, d)[:, 5:5 + N], r(B, 2 * N, H, d)[:, ::2], r(B, N, 3 * H, d)[:, :, H:2 * H]):
+        want, dense = torch.empty(B, N, H, d, device="cuda", dtype=x.dtype), x.contiguous()
+        xd.xdit_rope(dense, cos, sin, want)
+        for out in (torch.zeros(B, H, N, d, device="cuda", dtype=x.dtype).transpose(1, 2),
+                    torch.zeros(B, N, 3 * H, d, device="cuda", dtype=x.dtype)[:, :, :H]):
+            xd.xdit_rope(x, cos, sin, out)
+            assert torch.equal(out, want)
+    # only the view's elements are written
+    buf = torch.zeros(B, N, 3 * H, d, device="cuda", dtype=torch.bfloat16)
+    xd.xdit_rope(dense, cos, sin, buf[:, :, H:2 * H])
+    assert not buf[:, :, :H].any() and not buf[:, :, 2 * H:].any() and torch.equal(buf[:, :, H:2 * H], want)
+
+
+# -- norms --------------------------------------------------------------------
+CASES = [  # B, N, H, Hk, d, rot, weights
+    (2, 37, 3, 3, 64, 64, "f32"), (1, 1, 24, 24, 128, 128, "bf16"), (2, 130, 17, 5, 72, 72, "bf16"), (1, 300, 24, 0, 128, 56, "f32"),
+    (3, 5, 1, 2, 72, 0, None), (1, 77, 48, 48, 64, 32, "bf16"), (2, 64, 33, 70, 128, 8, "f32"), (1, 2, 6, 6, 64, 24, None)]
+
+
+def _case(r, B, N, H, Hk, d, rot, wt, norm, dtype, fused):
+    if fused:
+        qkv = r(B, N, H + 2 * Hk, d, dtype=dtype, scale=1.5, shift=0.4)
+        q, k = qkv[:, :, :H], qkv[:, :, H:H + Hk] if Hk else None
+    else:
+        q = r(B, N, H, d, dtype=dtype, scale=1.5, shift=0.4)
+        k = r(B, N, Hk, d, dtype=dtype, scale=1.5, shift=0.4) if Hk else None
+    w = dict(wq=None, wk=None, bq=None, bk=None)
+    if wt:
+        w["wq"] = r(d, dtype=wt, scale=0.3, shift=1.0)
+        w["wk"] = r(d, dtype=wt, scale=0.3, shift=1.0)
+        if norm == "layer":
+            w["bq"], w["bk"] = r(d, dtype=wt, scale=0.2), r(d, dtype=wt, scale=0.2)
+    cos, sin = r.angles(N, rot // 2) if rot else (None, None)
+    return q, k, w, cos, sin
+
+
+@pytest.mark.parametrize("fused", [False, True], ids=["apart", "fused"])
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_rope(dtype, norm, layout, fused):
+    torch = torch_mod()
+    r = Draws(11)
+    for case in CASES:
+        B, N, H, Hk, d, rot, wt = case
+        q, k, w, cos, sin = _case(r, *case, norm, dtype, fused)
+        new = lambda t: None if t is None else torch.full(t.shape, float("nan"), device="cuda", dtype=t.dtype)
+        qo, ko = new(q), new(k)
+        kw = dict(norm=norm, eps=1e-5, cos=cos, sin=sin, layout=layout)
+        xd.xdit_qk_norm_rope(q, k, qo, ko, **kw, **w)
+        for x, y, wn, bn in ((q, qo, "wq", "bq"), (k, ko, "wk", "bk")):
+            if x is None:
+                continue
+            args = _np(x), _np(w[wn]), _np(w[bn])
+            want = ref.forward(*args, _np32(cos), _np32(sin), norm, 1e-5, layout)
+            _close(_np(y), want, ref.forward_scale(*args, norm, 1e-5), dtype, f"{case} {wn}")
+        # in place, also where queries and keys are views of one buffer
+        xd.xdit_qk_norm_rope(q, k, q, k, **kw, **w)
+        assert torch.equal(q, qo) and (k is None or torch.equal(k, ko)), case
+
+
+@pytest.mark.parametrize("fused", [False, True], ids=["apart", "fused"])
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_rope_bwd(dtype, norm, layout, fused):
+    torch = torch_mod()
+    r = Draws(12)
+    for case in CASES:
+        B, N, H, Hk, d, rot, wt = case
+        q, k, w, cos, sin = _case(r, *case, norm, dtype, fused)
+        gq, gk = r(B, N, H, d, dtype=dtype), r(B, N, Hk, d, dtype=dtype) if Hk else None
+        new = lambda t: None if t is None else torch.full(t.shape, float("nan"), device="cuda", dtype=t.dtype)
+        dq, dk = new(q), new(k)
+        grad = {n: torch.full((d,), float("nan"), device="cuda") if (Hk or n.endswith("q")) and (norm == "layer" or n[1] == "w")
+                else None for n in ("dwq", "dwk", "dbq", "dbk")}
+        ws = torch.full((xd.qk_norm_rope_bwd_workspace_bytes(q, k) // 4,), float("nan"), device="cuda")
+        kw = dict(norm=norm, eps=1e-5, wq=w["wq"], wk=w["wk"], cos=cos, sin=sin, layout=layout)
+        xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, dq, dk, **kw, **grad, workspace=ws)
+        for x, g, dx, n in ((q, gq, dq, "q"), (k, gk, dk, "k")):
+            if x is None:
+                continue
+            X, G = _np(x), _np(g)
+            want, dw, db, scale = ref.backward(X, _np(w["w" + n]), G, _np32(cos), _np32(sin), norm, 1e-5, layout)
+            _close(_np(dx), want, scale, dtype, f"{case} d{n}")
+            sw, sb = ref.sums_scale(X, G, norm, 1e-5)
+            # the mean's subtraction costs what the largest value of a head has
+            sw = sw + (2 * np.abs(G).max(-1, keepdims=True) * np.abs(X).max(-1, keepdims=True)
+                       * ref.normalised(X, norm, 1e-5)[1]).sum((0, 1, 2))
+            _close(_np32(grad["dw" + n]), dw, sw, "f32", f"{case} dw{n}", steps=320)
+            if norm == "layer":
+                _close(_np32(grad["db" + n]), db, sb, "f32", f"{case} db{n}", steps=320)
+        # without the weights' gradients, no workspace; the gradient in place
+        xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, gq, gk, **kw)
+        assert torch.equal(gq, dq) and (gk is None or torch.equal(gk, dk)), case
+
+
+def test_heads_of_zeros_and_one_value():
+    """A head of zeros stays zero (eps alone is under the root) and its gradient
+    is finite; a head of one repeated value is what each norm makes of it."""
+    torch = torch_mod()
+    x = torch.zeros(1, 4, 2, 64, device="cuda")
+    x[:, 2:] = 3.0
+    g = torch.ones_like(x)
+    for norm, v in (("rms", 3.0 / np.sqrt(9.0 + 1e-6)), ("layer", 0.0)):
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        xd.xdit_qk_norm_rope(x, None, y, None, norm=norm, eps=1e-6)
+        assert not y[:, :2].any() and np.allclose(y[:, 2:].cpu().numpy(), v, rtol=1e-6)
+        xd.xdit_qk_norm_rope_bwd(x, None, g, None, dx, None, norm=norm, eps=1e-6)
+        assert torch.isfinite(dx).all()
+    bad = x.clone()
+    bad[0, 1, 0, 5] = float("nan")  # stays in its head
+    xd.xdit_qk_norm_rope(bad, None, y, None, norm="layer", eps=1e-6)
+    assert torch.isnan(y[0, 1, 0]).all() and not torch.isnan(y[0, 1, 1]).any() and not torch.isnan(y[0, 0]).any()
+
+
+def test_no_rows():
+    """No rows leave zero gradients of the weights, and write nothing else."""
+    torch = torch_mod()
+    for B, N in ((1, 0), (0, 7)):
+        x = torch.empty(B, N, 3, 64, device="cuda", dtype=torch.bfloat16)
+        dw, db = (torch.full((64,), float("nan"), device="cuda") for _ in range(2))
+        xd.xdit_qk_norm_rope(x, None, x.clone(), None)
+        ws = torch.empty(max(1, xd.qk_norm_rope_bwd_workspace_bytes(x, None)), device="cuda", dtype=torch.uint8)
+        xd.xdit_qk_norm_rope_bwd(x, None, x.clone(), None, x.clone(), None, norm="layer", dwq=dw, dbq=db, workspace=ws)
+        assert not dw.any() and not db.any()
+
+
+def test_many_rows_for_each_wave():
+    """More tokens than waves: every row is done, and the weights' gradients
+    hold them all (exactly: rows of ones and small whole gradients)."""
+    torch = torch_mod()
+    B, N, H, d = 2, 9001, 6, 128
+    x = torch.ones(B, N, H, d, device="cuda", dtype=torch.bfloat16)
+    g = torch.zeros(B, N, H, d, device="cuda", dtype=torch.bfloat16)
+    g[..., ::2] = 1.0
+    g[..., 1::4] = -1.0
+    dw = torch.empty(d, device="cuda")
+    dx = torch.full_like(x, float("nan"))
+    ws = torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(x, None), device="cuda", dtype=torch.uint8)
+    xd.xdit_qk_norm_rope_bwd(x, None, g, None, dx, None, norm="rms", eps=0.0, dwq=dw, workspace=ws)
+    assert torch.equal(dw, g[0, 0, 0].float() * (B * N * H))
+    # dx = g - mean(g) at unit values
+    assert torch.equal(dx, (g.float() - g.float().mean(-1, keepdim=True)).bfloat16())
+    first = dw.clone()
+    xd.xdit_qk_norm_rope_bwd(x, None, torch.randn_like(g), None, dx, None, norm="rms", eps=0.0, dwq=dw, workspace=ws)
+    again = dw.clone()
+    assert not torch.equal(first, again)
+
+
+def test_streams_and_graphs():
+    """On a stream of its own, and captured and replayed with other inputs in
+    the same buffers, between eager calls on a second workspace."""
+    torch = torch_mod()
+    r = Draws(13)
+    B, N, H, d = 1, 700, 24, 64
+    q, k, gq, gk = (r(B, N, H, d) for _ in range(4))
+    wq, wk = r(d, dtype="f32", shift=1.0, scale=0.2), r(d, dtype="f32", shift=1.0, scale=0.2)
+    cos, sin = torch.empty(N, d // 2, device="cuda"), torch.empty(N, d // 2, device="cuda")
+    pos = torch.arange(N, device="cuda")[:, None]
+
+    def call(bufs, ws):
+        qo, ko, dq, dk, dwq, dwk = bufs
+        xd.xdit_rope_table(pos, [d], cos, sin)
+        xd.xdit_qk_norm_rope(q, k, qo, ko, wq=wq, wk=wk, cos=cos, sin=sin)
+        xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, dq, dk, wq=wq, wk=wk, cos=cos, sin=sin, dwq=dwq, dwk=dwk, workspace=ws)
+
+    def bufs():
+        return [torch.zeros_like(q) for _ in range(4)] + [torch.zeros(d, device="cuda") for _ in range(2)]
+
+    ws = [torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(q, k), device="cuda", dtype=torch.uint8) for _ in range(2)]
+    eager, side, cap = bufs(), bufs(), bufs()
+    call(eager, ws[0])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(side, ws[1])
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(eager, side):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(cap, ws[1])
+    for i in range(4):
+        q.copy_(r(B, N, H, d))
+        gk.copy_(r(B, N, H, d))
+        for t in cap:
+            t.zero_()
+        graph.replay()
+        call(eager, ws[0])
+        torch.cuda.synchronize()
+        for a, b in zip(eager, cap):
+            assert torch.equal(a, b), f"replay {i}"
+
+
+def test_both_call_paths_agree(monkeypatch):
+    torch = torch_mod()
+    nat = xd._load_native()
+    assert nat
+    r = Draws(14)
+    B, N, H, Hk, d = 2, 33, 6, 3, 72
+    qkv = r(B, N, H + 2 * Hk, d)
+    q, k, gq, gk = qkv[:, :, :H], qkv[:, :, H:H + Hk], r(B, N, H, d), r(B, N, Hk, d)
+    wq, wk, bq, bk = (r(d, shift=1.0) for _ in range(4))
+    cos, sin = r.angles(B, N, 12)
+
+    def calls():
+        out = [torch.zeros(B, N, H, d, device="cuda", dtype=torch.bfloat16) for _ in range(3)]
+        out += [torch.zeros(B, N, Hk, d, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+        out += [torch.zeros(d, device="cuda") for _ in range(4)]
+        ws = torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(q, k), device="cuda", dtype=torch.uint8)
+        xd.xdit_rope(q, cos, sin, out[0], layout="half", transpose=True)
+        xd.xdit_qk_norm_rope(q, k, out[1], out[3], norm="layer", wq=wq, wk=wk, bq=bq, bk=bk, cos=cos, sin=sin, layout="half")
+        xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, out[2], out[4], norm="layer", wq=wq, wk=wk, cos=cos, sin=sin, layout="half",
+                                 dwq=out[5], dwk=out[6], dbq=out[7], dbk=out[8], workspace=ws)
+        return out
+
+    class Taken:
+        def __init__(self):
+            self.names = []
+
+        def __getattr__(self, name):
+            def call(*a):
+                rc = getattr(nat, name)(*a)
+                self.names.append((name, rc))
+                return rc
+            return call
+
+    rec = Taken()
+    monkeypatch.setattr(xd, "_native", rec)
+    fast = calls()
+    assert rec.names == [("rope", 0), ("qk_norm_rope", 0), ("qk_norm_rope_bwd", 0)]
+    monkeypatch.setattr(xd, "_native", False)
+    for a, b in zip(fast, calls()):
+        assert torch.equal(a, b)
+
+
+def test_refusals_on_the_gpu(monkeypatch):
+    """Both call paths refuse the same calls, and leave the outputs alone."""
+    torch = torch_mod()
+    nat = xd._load_native()
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, device="cuda", dtype=dt)
+    q, k, qo, ko = (z(1, 5, 2, 64) for _ in range(4))
+    c, w, f32 = z(5, 16, dt=torch.float32), z(64), torch.float32
+    ws = z(1 << 20, dt=torch.uint8)
+    norm, bwd = xd.xdit_qk_norm_rope, xd.xdit_qk_norm_rope_bwd
+    bad = [lambda: xd.xdit_rope(q, c, c, qo, layout="other"), lambda: xd.xdit_rope(q, c[:4], c[:4], qo),
+           lambda: xd.xdit_rope(q, c, c[:, :8].contiguous(), qo), lambda: xd.xdit_rope(q, c, None, qo),
+           lambda: xd.xdit_rope(q, z(5, 36, dt=f32), z(5, 36, dt=f32), qo), lambda: xd.xdit_rope(q, c, c, qo.float()),
+           lambda: xd.xdit_rope(q, z(5, 6, dt=f32), z(5, 6, dt=f32), qo), lambda: xd.xdit_rope(q.half(), c, c, qo.half()),
+           lambda: xd.xdit_rope(q[..., :32], c, c, qo[..., :32]), lambda: xd.xdit_rope(q, c, c, z(1, 1, 2, 64).expand(1, 5, 2, 64)),
+           lambda: xd.xdit_rope(z(6, 2, 64)[None, :5], c, c, z(1, 5, 2, 65)[..., 1:]),
+           lambda: norm(q, k, qo, ko, norm="none"), lambda: norm(q, k, qo, ko, bq=w), lambda: norm(q, k, qo, ko, eps=-1.0),
+           lambda: norm(q, k, qo, ko, eps=float("nan")), lambda: norm(q, k, qo, None), lambda: norm(q, None, qo, ko),
+           lambda: norm(q, k, qo, qo), lambda: norm(q, k, k, ko), lambda: norm(q, k, qo, ko, wq=w, wk=w.float()),
+           lambda: norm(q, k, qo, ko, wq=w[:32]), lambda: norm(q, k, qo, ko, cos=c), lambda: norm(q, q.cpu(), qo, ko),
+           lambda: norm(q, k, qo[:, 1:], ko), lambda: norm(z(1, 6, 2, 64)[:, :5], k, z(1, 6, 2, 64)[:, 1:], None),
+           lambda: bwd(q, k, q, k, qo, ko, dwq=z(64, dt=f32)), lambda: bwd(q, k, q, k, qo, ko, dwq=z(64), workspace=ws),
+           lambda: bwd(q, k, q, k, qo, ko, dbq=z(64, dt=f32), workspace=ws),
+           lambda: bwd(q, k, q, k, qo, ko, dwq=z(64, dt=f32), workspace=ws[:100]),
+           lambda: bwd(q, None, q, None, qo, None, dwk=z(64, dt=f32), workspace=ws),
+           lambda: bwd(q, k, q, k, qo, ko, dwq=(x := z(64, dt=f32)), dwk=x, workspace=ws)]
+    for path in (nat, False):
+        monkeypatch.setattr(xd, "_native", path)
+        for i, f in enumerate(bad):
+            with pytest.raises(xd.XditError):
+                f()
+                pytest.fail(f"call {i} was taken")
+    # one row shifted against itself within a buffer is no in-place call
+    buf = z(1, 6, 2, 64)
+    with pytest.raises(xd.XditError):
+        xd.xdit_rope(buf[:, :5], c, c, buf[:, 1:])
+    torch.cuda.synchronize()
+    assert not qo.any() and not ko.any()
