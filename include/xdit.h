@@ -61,6 +61,9 @@ enum { XDIT_PAIRS_INTERLEAVED = 0, XDIT_PAIRS_HALF = 1 };
 /* Scaling of a rotary table's frequencies (xdit_rope_table). */
 enum { XDIT_ROPE_NONE = 0, XDIT_ROPE_LINEAR = 1, XDIT_ROPE_NTK = 2, XDIT_ROPE_RAMP = 3 };
 
+/* Gradients of xdit_chunk_attn_bwd that are float32 sums to add to. */
+enum { XDIT_ACCUM_DQ = 1, XDIT_ACCUM_DKV = 2 };
+
 /* Upper bound on the axes of one rotary table. */
 #define XDIT_MAX_AXES 4
 
@@ -318,6 +321,39 @@ int xdit_stage_step(const void* x, const void* wq, const void* wk, const void* w
                     void* kv_buf, int64_t patch_off, int64_t patch_len, void* q, void* k, void* v,
                     void* o, void* y, int64_t batch, int64_t seq_len, int64_t heads,
                     int64_t head_dim, int64_t hidden, int32_t dtype);
+
+/*
+ * Gradients of chunk attention.  With s_ij = (q_i . k_j) / sqrt(d):
+ *   P_ij = exp(s_ij - lse_i),  D_i = dout_i . out_i - dlse_i
+ *   dv_j = sum_i P_ij dout_i
+ *   dk_j = sum_i P_ij (dout_i . v_j - D_i) q_i / sqrt(d)
+ *   dq_i = sum_j P_ij (dout_i . v_j - D_i) k_j / sqrt(d)
+ * out and lse are what xdit_chunk_attn gave for these chunk's keys, dlse the
+ * gradient of that lse: the chunk's partial is then merged further.  Or out
+ * and lse are those of all chunks of a sequence (merged, or a ring's running
+ * state) with dout their gradient: the call then gives this chunk's dk and dv
+ * and its part of dq, and the parts of all chunks add up (XDIT_ACCUM_DQ).
+ *   q, out, dout [B, q_len, H, d];  k, v [B, kv_len, H, d]
+ *   lse, dlse    [B, H, q_len] float32; dlse may be NULL (zeros)
+ *   dq           [B, q_len, H, d], dk, dv [B, kv_len, H, d], written; with
+ *                XDIT_ACCUM_DQ dq, with XDIT_ACCUM_DKV dk and dv, is a float32
+ *                tensor that the gradient is added to (dk and dv travel with
+ *                their chunk through the ring)
+ *   workspace    xdit_chunk_attn_bwd_workspace_bytes(...) bytes, 256-byte
+ *                aligned, overlapping nothing; its contents on entry do not
+ *                matter.  Calls that overlap in time need one each.
+ * A row whose lse is -inf (it met no key) has no part in any gradient; its out
+ * is not read, its dout must be finite.  kv_len = 0 gives dq = 0, q_len = 0
+ * gives dk = dv = 0.  Sums are float32 and their order is fixed: the same call
+ * gives the same bits.  bf16 calls round P and the scores' gradient to bf16 as
+ * operands of the matrix cores.  No output overlaps another tensor.
+ */
+int64_t xdit_chunk_attn_bwd_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads,
+                                            int64_t head_dim, int32_t dtype);
+int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,
+                        const void* dout, const float* dlse, void* dq, void* dk, void* dv, int32_t accum,
+                        void* workspace, int64_t workspace_bytes, int64_t batch, int64_t q_len,
+                        int64_t kv_len, int64_t heads, int64_t head_dim, int32_t dtype);
 
 /*
  * The table of a rotary position embedding: of every row, the cosines and

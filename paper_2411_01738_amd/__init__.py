@@ -17,7 +17,7 @@ from __future__ import annotations
 import ctypes
 import warnings
 
-from ._lib import (LAYOUTS, NORMS, SCALINGS, XDIT_BF16, XDIT_F32, XDIT_I64, XDIT_MAX_AXES, XDIT_MAX_PARTIALS,
+from ._lib import (LAYOUTS, NORMS, SCALINGS, XDIT_ACCUM_DKV, XDIT_ACCUM_DQ, XDIT_BF16, XDIT_F32, XDIT_I64, XDIT_MAX_AXES, XDIT_MAX_PARTIALS,
                    XDIT_MAX_RANGES, XDIT_MAX_SPLITS, Qk, RopeScaling, XditError, check, lib)
 
 __all__ = ["xdit_patch_attn", "xdit_patch_attn_ranges", "xdit_chunk_attn",
@@ -25,7 +25,8 @@ __all__ = ["xdit_patch_attn", "xdit_patch_attn_ranges", "xdit_chunk_attn",
            "xdit_patch_attn_split", "xdit_chunk_attn_split_noalloc",
            "split_workspace_bytes", "xdit_lse_merge",
            "xdit_kv_update", "xdit_stage_step", "xdit_rope_table", "xdit_rope", "xdit_qk_norm_rope",
-           "xdit_qk_norm_rope_bwd", "qk_norm_rope_bwd_workspace_bytes", "set_stream", "XditError", "XDIT_MAX_PARTIALS", "XDIT_MAX_RANGES",
+           "xdit_qk_norm_rope_bwd", "qk_norm_rope_bwd_workspace_bytes", "xdit_chunk_attn_bwd",
+           "chunk_attn_bwd_workspace_bytes", "set_stream", "XditError", "XDIT_MAX_PARTIALS", "XDIT_MAX_RANGES",
            "version"]
 
 
@@ -547,3 +548,53 @@ def xdit_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, norm: str = "rms", eps: 
     _use_current_stream()
     check(lib().xdit_qk_norm_rope_bwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk),
                                       _ptr(dwq), _ptr(dwk), _ptr(dbq), _ptr(dbk), wp, wb))
+
+
+# -- the attention's gradients --------------------------------------------------
+def chunk_attn_bwd_workspace_bytes(q, kv_len: int) -> int:
+    """Bytes of workspace that xdit_chunk_attn_bwd needs for queries shaped like
+    q [B, Nq, H, d] over kv_len keys."""
+    B, Nq, H, d = q.shape
+    n = lib().xdit_chunk_attn_bwd_workspace_bytes(B, Nq, int(kv_len), H, d, _dtype_code(q))
+    if n < 0:
+        raise XditError(-3, "xdit_chunk_attn_bwd_workspace_bytes rejected the sizes")
+    return int(n)
+
+
+def xdit_chunk_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, dlse=None, accum_dq: bool = False, accum_dkv: bool = False,
+                        workspace=None) -> None:
+    """Gradients dq [B, Nq, H, d], dk, dv [B, Nk, H, d] of xdit_chunk_attn's
+    inputs, given its out and lse, the gradient dout of out and, if any, dlse of
+    lse; or, given the out and lse of all chunks of a sequence and their dout,
+    this chunk's dk and dv and its part of dq.  accum_dq: dq is a float32 sum
+    that the part is added to; accum_dkv: dk and dv are.  workspace: a GPU
+    tensor of chunk_attn_bwd_workspace_bytes bytes."""
+    nat = _native if _native is not None else _load_native()
+    if nat and _done(nat.chunk_bwd(q, k, v, out, lse, dout, dq, dk, dv, dlse, accum_dq, accum_dkv, workspace)):
+        return
+    torch = _torch()
+    args = _chunk_args(q, k, v, out, lse)
+    if lse is None:
+        raise XditError(-1, "lse is required")
+    B, Nq, H, d = q.shape
+    for t, n, like, accum in ((dout, "dout", q, False), (dq, "dq", q, accum_dq), (dk, "dk", k, accum_dkv),
+                              (dv, "dv", k, accum_dkv)):
+        if t is None:
+            raise XditError(-1, f"{n} is required")
+        _dense(t, n, 4)
+        if tuple(t.shape) != tuple(like.shape):
+            raise XditError(-3, f"{n} has shape {tuple(t.shape)}, expected {tuple(like.shape)}")
+        if t.dtype != (torch.float32 if accum else q.dtype):
+            raise XditError(-2, f"{n} has dtype {t.dtype}, expected {torch.float32 if accum else q.dtype}")
+    _dense(dlse, "dlse", 3)
+    if dlse is not None and (dlse.dtype != torch.float32 or tuple(dlse.shape) != (B, H, Nq)):
+        raise XditError(-3, f"dlse must be float32 [B,H,Nq] = {(B, H, Nq)}")
+    for t, n in ((q, "q"), (k, "k"), (v, "v"), (out, "out"), (lse, "lse"), (dout, "dout"), (dq, "dq"), (dk, "dk"), (dv, "dv"),
+                 (dlse, "dlse"), (workspace, "workspace")):
+        if t is not None:
+            _on_device(t, n)
+    wp, wb = _workspace(workspace)
+    _use_current_stream()
+    check(lib().xdit_chunk_attn_bwd(*args[:5], _ptr(dout), _ptr(dlse), _ptr(dq), _ptr(dk), _ptr(dv),
+                                    (XDIT_ACCUM_DQ if accum_dq else 0) | (XDIT_ACCUM_DKV if accum_dkv else 0), wp, wb,
+                                    *args[5:]))

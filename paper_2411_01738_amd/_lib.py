@@ -24,6 +24,7 @@ NORMS = {"rms": 1, "layer": 2}
 LAYOUTS = {"interleaved": 0, "half": 1}
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
 XDIT_MAX_AXES = 4
+XDIT_ACCUM_DQ, XDIT_ACCUM_DKV = 1, 2
 XDIT_MAX_PARTIALS = 64
 XDIT_MAX_RANGES = 2
 XDIT_MAX_SPLITS = 16
@@ -69,6 +70,8 @@ SIGNATURES = {
     "xdit_kv_update": (ctypes.c_int, [_vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i32]),
     "xdit_stage_step": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp,
                                        _vp, _i64, _i64, _i64, _i64, _i64, _i32]),
+    "xdit_chunk_attn_bwd_workspace_bytes": (_i64, [_i64, _i64, _i64, _i64, _i64, _i32]),
+    "xdit_chunk_attn_bwd": (ctypes.c_int, [_vp] * 10 + [_i32, _vp, _i64] + [_i64] * 5 + [_i32]),
     "xdit_rope_table": (ctypes.c_int, [_vp, _i32, _i64, _i32, _vp, _f64, ctypes.POINTER(RopeScaling), _vp, _vp]),
     "xdit_rope": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i32, _i32, _i32, _i32]),
     "xdit_qk_norm_rope": (ctypes.c_int, [ctypes.POINTER(Qk), _vp, _vp, _vp, _vp]),

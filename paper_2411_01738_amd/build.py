@@ -19,7 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIBRARY = os.path.join(HERE, "libxdit.so")
 BINDING = os.path.join(HERE, "_binding.so")
-SOURCES = ["xdit_api.cpp", "layer_api.cpp", "norm_rope.hip", "attn_bf16.hip", "attn_w64.hip", "attn_f32.hip", "merge_update.hip"]
+SOURCES = ["xdit_api.cpp", "layer_api.cpp", "norm_rope.hip", "attn_bf16.hip", "attn_w64.hip", "attn_f32.hip", "merge_update.hip",
+           "attn_bwd.hip", "attn_bwd_f32.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,507 @@
+// Gradients of bf16 attention (chunk attention with O and LSE, possibly merged
+// with other chunks) on the gfx950 matrix cores.
+//
+// Per (batch, head), with s_ij = (q_i . k_j) / sqrt(d), the LSE l_i and output
+// o_i of the row (over all chunks), and the gradients g_i of o_i, e_i of l_i:
+//   P_ij  = exp(s_ij - l_i)
+//   D_i   = g_i . o_i - e_i
+//   dS_ij = P_ij (g_i . v_j - D_i)
+//   dV_j  = sum_i P_ij g_i
+//   dK_j  = sum_i dS_ij q_i / sqrt(d),  dQ_i = sum_j dS_ij k_j / sqrt(d)
+// The probabilities are computed again from the scores; nothing of size
+// queries x keys is stored.  P and dS are rounded to bf16 as operands of the
+// matrix cores (half a step, 2^-8 relative, each; the sums are float32).
+//
+// What bounds it: the matrix cores.  One sweep gives dK and dV (four products
+// of queries x keys x d), another dQ (three), seven in place of the five that
+// are needed: a single sweep would have to add its part of the other side's
+// gradient to memory for every tile, by atomics whose order changes the result
+// or through partials larger than the inputs.
+//
+// Work decomposition: one workgroup = kRows resident rows (keys of dK/dV,
+// queries of dQ) of one (batch, head), 4 waves of 32 rows each, whose two
+// operands stay in registers; the other side's two tensors stream through LDS
+// in tiles (memory straight into LDS, four stages, one barrier per tile):
+//   resident x streamed:  dK/dV: K, V x Q, G     dQ: Q, G x K, V
+//   X = T1 R1^T (scores), Y = T2 R2^T (g . v): a lane holds 16 streamed rows
+//   of one resident row;
+//   P and dS in these registers are at once the operands of the products that
+//   sum over streamed rows, A1^T += T2^T P and A2^T += T1^T dS, whose other
+//   operand is read from the same tiles by the transposing LDS read.
+// Layout of a tile in LDS, order of rows in a block (krow) and the padding of
+// d = 72 are those of attn_bf16.hip.  For dK/dV the rows' -l_i sqrt(d) and
+// -D_i come along with the tiles and are what X and Y start from; for dQ they
+// belong to the lane.
+#include "kernels.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+namespace xdit {
+namespace {
+
+#include "attn_common.h"
+
+struct BwdArgs {
+    const uint16_t* r1;   // resident operands, [B, Nr, H, D]
+    const uint16_t* r2;
+    const uint16_t* t1;   // streamed ones, [B, Nt, H, D]
+    const uint16_t* t2;
+    const float* rows;    // per (batch, head): [2][Nq] -l sqrt(d), -D
+    void* o1;             // dV (KV only)
+    void* o2;             // dK or dQ
+    float* part;          // splits > 1: float32 partials [splits][B, Nr, H, D] of o2, then of o1
+    int64_t part_elems;   // B * Nr * H * D
+    int B, H, Nr, Nt, r_tiles, splits;
+    int accum;            // o1, o2 are float32 sums to add to
+    float c2, scale;      // softmax scale * log2(e), softmax scale
+};
+
+constexpr int kRows = 128;
+
+template <int D, bool KV>
+struct BCfg {
+    static constexpr int NW = 4, THREADS = 64 * NW;
+    static constexpr int NB = D > 96 ? 1 : 2;           // 32-row blocks of a tile
+    static constexpr int BN = 32 * NB;                  // streamed rows per tile
+    static constexpr int CH = D / 8, ROWB = 16 * CH;    // 16-byte chunks and bytes of a row
+    static constexpr int KSTEPS = (D + 15) / 16;
+    static constexpr int DBLK = D / 32;
+    static constexpr bool TAIL = D % 32 != 0;           // d = 72: dims 64..71 on the 16x16x32 instruction
+    static constexpr bool PERM = CH != 8;
+    static constexpr int E_ROWS = PERM ? 2 : 8;         // rows between the two half k-steps of a transposing read
+    __device__ static constexpr int swz(int r) {
+        if constexpr (CH == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+        else if constexpr (CH == 16) return r & 15;
+        else return 0;
+    }
+    static constexpr bool SWIZZLED = CH == 8 || CH == 16;
+    static constexpr int REGION = BN * ROWB;            // one tile of one tensor
+    static constexpr int NST = 4;
+    static constexpr int T2BASE = NST * REGION;         // T1's regions, then T2's
+    static constexpr int ROWBASE = 2 * NST * REGION;    // then the rows' scalars (KV)
+    static constexpr int ROWREGION = KV ? 8 * BN : 0;
+    static constexpr int LDS_BYTES = ROWBASE + NST * ROWREGION;
+    static constexpr int DMA_PER_TILE = REGION / 1024;
+    static constexpr int DMA_PER_WAVE = (DMA_PER_TILE + NW - 1) / NW;
+    static_assert(REGION % 1024 == 0 && LDS_BYTES <= kLdsBytes / 2, "two workgroups per CU");
+};
+
+template <int D, bool KV>
+__global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
+    using C = BCfg<D, KV>;
+    constexpr int NST = C::NST, NB = C::NB, BN = C::BN, KSTEPS = C::KSTEPS, DBLK = C::DBLK, NW = C::NW;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS_BYTES];
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 31, hf = lane >> 5;
+    const int logical = xcd_remap(blockIdx.x, gridDim.x);
+    const int sp = logical % a.splits, pair = logical / a.splits;
+    const int rt = pair % a.r_tiles, bh = pair / a.r_tiles;
+    const int hh = bh % a.H, b = bh / a.H;
+    const uint32_t rowb = (uint32_t)a.H * D * 2, headb = (uint32_t)hh * D * 2;
+    const int64_t rs = (int64_t)a.H * D, headoff = (int64_t)hh * D;
+    const uint32_t lds_u32 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+
+    // this workgroup's tiles of the sweep
+    const int all_tiles = (a.Nt + BN - 1) / BN;
+    const int tb = (int)((int64_t)all_tiles * sp / a.splits);
+    const int ntiles = (int)((int64_t)all_tiles * (sp + 1) / a.splits) - tb;
+
+    auto rows_rsrc = [&](const uint16_t* base, int64_t n, int row0) -> Rsrc {
+        return rsrc(base + ((int64_t)b * n + row0) * rs + headoff, n > row0 ? (uint32_t)(n - row0) * rowb - headb : 0u);
+    };
+
+    // resident operands: row `row` of this wave, chunk 2kk + hf; chunks past d
+    // and rows past the end read as zero
+    const int row = rt * kRows + wave * 32 + c;
+    bf16x8 r1[KSTEPS], r2[KSTEPS];
+    {
+        const Rsrc q1 = rows_rsrc(a.r1, a.Nr, rt * kRows), q2 = rows_rsrc(a.r2, a.Nr, rt * kRows);
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; ++kk) {
+            const uint32_t off = 2 * kk + hf < C::CH ? (uint32_t)(wave * 32 + c) * rowb + 32 * kk + 16 * hf : kOOB;
+            r1[kk] = __builtin_bit_cast(bf16x8, bload(q1, off));
+            r2[kk] = __builtin_bit_cast(bf16x8, bload(q2, off));
+        }
+    }
+    // the resident row's own -l log2(e) and -D (dQ)
+    float nl = 0.f, nd = 0.f;
+    if constexpr (!KV) {
+        const float* rows = a.rows + (int64_t)bh * 2 * a.Nr;
+        if (row < a.Nr) {
+            nl = rows[row] * a.c2;
+            nd = rows[a.Nr + row];
+        }
+    }
+
+    // tile loads: piece n of this wave fills chunks 64 ins .. of a tile; chunk
+    // p is row p / CH, logical chunk (p % CH) ^ swz(row)
+    uint32_t dma_off[C::DMA_PER_WAVE];
+#pragma unroll
+    for (int n = 0; n < C::DMA_PER_WAVE; ++n) {
+        const int p = 64 * (wave + n * NW) + lane;
+        const int r = p / C::CH;
+        dma_off[n] = (uint32_t)r * rowb + 16 * ((p % C::CH) ^ C::swz(r));
+    }
+    auto load_tile = [&](int t, int s) {
+        const int lo = (tb + t) * BN;
+        const Rsrc q1 = rows_rsrc(a.t1, a.Nt, lo), q2 = rows_rsrc(a.t2, a.Nt, lo);
+#pragma unroll
+        for (int n = 0; n < C::DMA_PER_WAVE; ++n) {
+            const int ins = wave + n * NW;
+            if (C::DMA_PER_TILE % NW == 0 || ins < C::DMA_PER_TILE) {
+                dma16(q1, lds + s * C::REGION + 1024 * ins, dma_off[n]);
+                dma16(q2, lds + C::T2BASE + s * C::REGION + 1024 * ins, dma_off[n]);
+            }
+        }
+        if constexpr (KV) {
+            // slot x of a block holds the row that accumulator row x is: 32
+            // values of -l sqrt(d), then 32 of -D, per block; the last wave's work
+            if (wave == NW - 1) {
+                const Rsrc qr = rsrc(a.rows + (int64_t)bh * 2 * a.Nt, (uint32_t)a.Nt * 8);
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb) {
+                    const int j = lo + 32 * kb + krow<C::PERM>(c);
+                    const uint32_t off = j < a.Nt ? 4u * (uint32_t)(j + (hf ? a.Nt : 0)) : kOOB;
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_void*)(lds + C::ROWBASE + s * C::ROWREGION + 256 * kb), 4,
+                                                             off, 0, 0, 0);
+                }
+            }
+        }
+    };
+    // at most the loads of the N youngest tiles are in flight
+    constexpr int LOADS = 2 * (C::DMA_PER_TILE / NW);                       // of a wave without extras
+    constexpr int FIRST = LOADS + (C::DMA_PER_TILE % NW ? 2 : 0);           // waves that take a left-over piece
+    constexpr int LAST = LOADS + (KV ? NB : 0);
+    static_assert(C::DMA_PER_TILE % NW <= 1, "one wave takes a left-over piece");
+    auto wait_tiles = [&](auto n_c) {
+        constexpr int N = decltype(n_c)::value;
+        if (FIRST != LOADS && wave == 0) wait_vmem<N * FIRST>();
+        else if (LAST != LOADS && wave == NW - 1) wait_vmem<N * LAST>();
+        else wait_vmem<N * LOADS>();
+    };
+
+    // LDS addresses of this lane's operand reads in stage 0 (T1's region)
+    uint32_t kaddr[KSTEPS];
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; ++kk) {
+        // a chunk past d meets zeros of the resident operand: any finite values do
+        const int r = krow<C::PERM>(c), lc = 2 * kk + hf < C::CH ? 2 * kk + hf : C::CH - 1;
+        kaddr[kk] = lds_u32 + r * C::ROWB + 16 * (lc ^ C::swz(r));
+    }
+    const int gi = lane & 15, grp = lane >> 4;
+    constexpr int NE = C::SWIZZLED ? 2 : 1, NDB = C::SWIZZLED ? DBLK : 1;
+    uint32_t vaddr[NDB][NE];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+            const int dim = 32 * db + 16 * (grp & 1) + 4 * (gi & 3);
+            const int r = krow<C::PERM>(4 * hf + (gi >> 2)) + C::E_ROWS * e;
+            vaddr[db][e] = lds_u32 + r * C::ROWB + 16 * ((dim >> 3) ^ C::swz(r)) + 2 * (dim & 7);
+        }
+    // tail (d = 72): group g reads dims 64..71 of the rows of k-step g & 1, half g >> 1
+    uint32_t taddr = 0;
+    if constexpr (C::TAIL) {
+        const int r = krow<C::PERM>(4 * (grp >> 1) + (gi >> 2)) + 16 * (grp & 1);
+        taddr = lds_u32 + r * C::ROWB + 2 * (32 * DBLK + 4 * (gi & 1));
+    }
+
+    f32x16 acc1[KV ? DBLK : 1], acc2[DBLK];
+    f32x4 tail1[2] = {}, tail2[2] = {};
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db) {
+        if constexpr (KV) acc1[db] = f32x16{};
+        acc2[db] = f32x16{};
+    }
+
+    // A^T += T^T W over one 32-row block, W = w[0], w[1] (16 rows each)
+    auto gather = [&](auto off_c, uint32_t so, const bf16x8 (&w)[2], f32x16* acc, f32x4* tail) {
+        constexpr int OFF = decltype(off_c)::value;
+        u32x2 vr[2][DBLK][2], vt[2];
+        static_for<0, 2>([&](auto ksc) {
+            constexpr int ks = decltype(ksc)::value;
+            static_for<0, DBLK>([&](auto dbc) {
+                constexpr int db = decltype(dbc)::value;
+                if constexpr (C::SWIZZLED) {
+                    vr[ks][db][0] = tr_read<OFF + 16 * ks * C::ROWB>(vaddr[db][0] + so);
+                    vr[ks][db][1] = tr_read<OFF + 16 * ks * C::ROWB>(vaddr[db][NE - 1] + so);
+                } else {
+                    vr[ks][db][0] = tr_read<OFF + 16 * ks * C::ROWB + 64 * db>(vaddr[0][0] + so);
+                    vr[ks][db][1] = tr_read<OFF + (16 * ks + C::E_ROWS) * C::ROWB + 64 * db>(vaddr[0][0] + so);
+                }
+            });
+        });
+        if constexpr (C::TAIL) {
+            vt[0] = tr_read<OFF>(taddr + so);
+            vt[1] = tr_read<OFF + C::E_ROWS * C::ROWB>(taddr + so);
+        }
+        constexpr int T = C::TAIL ? 2 : 0;
+        static_for<0, 2>([&](auto ksc) {
+            constexpr int ks = decltype(ksc)::value;
+            static_for<0, DBLK>([&](auto dbc) {
+                constexpr int db = decltype(dbc)::value;
+                lds_wait_upto<2 * (DBLK * (2 - ks) - db - 1) + T>(vr[ks][db][0], vr[ks][db][1]);
+                const u32x4 v4 = {vr[ks][db][0][0], vr[ks][db][0][1], vr[ks][db][1][0], vr[ks][db][1][1]};
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v4), w[ks], acc[db], 0, 0, 0);
+            });
+        });
+        if constexpr (C::TAIL) {
+            lds_wait_upto<0>(vt[0], vt[1]);
+            const u32x4 x = __builtin_bit_cast(u32x4, w[0]), y = __builtin_bit_cast(u32x4, w[1]);
+            u32x4 b0, b1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const auto r = __builtin_amdgcn_permlane16_swap(x[i], y[i], false, false);
+                b0[i] = r[0];
+                b1[i] = r[1];
+            }
+            const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{vt[0][0], vt[0][1], vt[1][0], vt[1][1]});
+            tail[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b0), tail[0], 0, 0, 0);
+            tail[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b1), tail[1], 0, 0, 0);
+        }
+    };
+
+    // tile t in stage s
+    auto block = [&](int t, int s, auto kb_c, auto mask_c) {
+        constexpr int kb = decltype(kb_c)::value;
+        constexpr uint32_t BO = 32 * kb * C::ROWB;
+        const uint32_t so = (uint32_t)(s * C::REGION);
+        f32x16 x = {}, y = {};
+        if constexpr (KV) {
+            const uint32_t ra = lds_u32 + C::ROWBASE + (uint32_t)(s * C::ROWREGION) + 256 * kb + 16 * hf;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 xi = lds_ld<f32x4>(ra + 32 * g), yi = lds_ld<f32x4>(ra + 128 + 32 * g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[4 * g + i] = xi[i], y[4 * g + i] = yi[i];
+            }
+        }
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; ++kk) {
+            const bf16x8 k1 = lds_ld<bf16x8>(kaddr[kk] + so + BO);
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, r1[kk], x, 0, 0, 0);
+            const bf16x8 k2 = lds_ld<bf16x8>(kaddr[kk] + so + BO + C::T2BASE);
+            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k2, r2[kk], y, 0, 0, 0);
+        }
+        bf16x8 pb[2], zb[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            float p[8], z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = 8 * ks + e;
+                if constexpr (KV) {
+                    p[e] = __builtin_amdgcn_exp2f(x[i] * a.c2);
+                    z[e] = p[e] * y[i];
+                } else {
+                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c2, nl));
+                    if constexpr (decltype(mask_c)::value) {
+                        const int j = (tb + t) * BN + 32 * kb + krow<C::PERM>(8 * (i >> 2) + 4 * hf + (i & 3));
+                        if (j >= a.Nt) p[e] = 0.f;
+                    }
+                    z[e] = p[e] * (y[i] + nd);
+                }
+            }
+            u32x4 pw, zw;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (KV) pw[w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
+                zw[w] = pack_bf16x2(z[2 * w], z[2 * w + 1]);
+            }
+            if constexpr (KV) pb[ks] = __builtin_bit_cast(bf16x8, pw);
+            zb[ks] = __builtin_bit_cast(bf16x8, zw);
+        }
+        // d = 72: T2's regions end past a 16-bit offset, so its base is added
+        if constexpr (KV) gather(std::integral_constant<int, (int)BO>{}, so + C::T2BASE, pb, acc1, tail1);
+        gather(std::integral_constant<int, (int)BO>{}, so, zb, acc2, tail2);
+    };
+    auto tile = [&](int t, auto mask_c) {
+        const int s = t % NST;
+        static_for<0, NB>([&](auto kb_c) { block(t, s, kb_c, mask_c); });
+    };
+
+    if (ntiles > 0) {
+        // the first NST-1 tiles load whether or not there are that many (past
+        // the end they read zeros, into stages nobody reads)
+#pragma unroll
+        for (int t = 0; t < NST - 1; ++t) load_tile(t, t);
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; ++kk) asm volatile("" : "+v"(r1[kk]), "+v"(r2[kk]));
+        asm volatile("" : "+v"(nl), "+v"(nd));
+        for (int t = 0; t < ntiles; ++t) {
+            // tile t has landed (two younger may be in flight) in every wave, and
+            // every wave is done with tile t - 1, whose stage takes tile t + NST - 1
+            wait_tiles(std::integral_constant<int, NST - 2>{});
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            load_tile(t + NST - 1, (t + NST - 1) % NST);
+            if (!KV && (tb + t + 1) * BN > a.Nt) tile(t, std::true_type{});
+            else tile(t, std::false_type{});
+        }
+    }
+    wait_vmem<0>();
+
+    // Results: lane c holds resident row 32 wave + c, dims 32db + 8g + 4hf + i;
+    // the tail's lanes row 32 wave + 16h + (lane & 15), dims 64 + 4 (lane >> 4) + i
+    auto put = [&](void* dst, int64_t part0, int r, int dim, f32x4 v) {
+        if (r >= a.Nr) return;
+        const int64_t at = ((int64_t)b * a.Nr + r) * rs + headoff + dim;
+        if (a.splits > 1) {
+            *(f32x4*)(a.part + part0 + (int64_t)sp * a.part_elems + at) = v;
+        } else if (a.accum) {
+            f32x4* p = (f32x4*)((float*)dst + at);
+            *p = *p + v;
+        } else {
+            *(u32x2*)((uint16_t*)dst + at) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        }
+    };
+    auto result = [&](void* dst, int64_t part0, const f32x16* acc, const f32x4* tail, float f) {
+#pragma unroll
+        for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                put(dst, part0, row, 32 * db + 8 * g + 4 * hf,
+                    f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]} * f);
+        if constexpr (C::TAIL)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (grp < 2) put(dst, part0, rt * kRows + wave * 32 + 16 * h + gi, 32 * DBLK + 4 * grp, tail[h] * f);
+    };
+    result(a.o2, 0, acc2, tail2, a.scale);
+    if constexpr (KV) result(a.o1, a.splits * a.part_elems, acc1, tail1, 1.f);
+}
+
+// Per query row: -l sqrt(d) and -D = e - g . o.  A row whose l is -inf (no
+// key) gives -inf and 0: its probabilities are 0, and its o is not read.
+// One row of a head per L lanes; a wave's rows are consecutive rows of one head.
+struct RowsArgs {
+    const char* out;
+    const char* dout;
+    const float* lse;
+    const float* dlse;
+    float* rows;
+    int H, Nq, blocks;  // blocks of rows per head
+    float root;         // sqrt(d)
+};
+
+template <int D, int ES>
+__global__ __launch_bounds__(256) void bwd_rows_kernel(RowsArgs a) {
+    constexpr int CH = D * ES / 16;                       // 16-byte chunks of a row
+    constexpr int L = CH <= 8 ? 8 : CH <= 16 ? 16 : 32;   // lanes of a row
+    constexpr int R = 256 / L;                            // rows at a time
+    const int p = threadIdx.x % L, r = threadIdx.x / L;
+    const int bh = blockIdx.x / a.blocks, blk = blockIdx.x % a.blocks;
+    const int hh = bh % a.H;
+    const int64_t b = bh / a.H;
+    const int i = blk * R + r;
+    if (i >= a.Nq) return;
+    const int64_t at = (((b * a.Nq + i) * a.H + hh) * CH + p) * 16;
+    const int64_t li = (int64_t)bh * a.Nq + i;
+    const float l = a.lse[li];
+    float s = 0.f;
+    if (p < CH) {
+        const u32x4 x = *(const u32x4*)(a.out + at), g = *(const u32x4*)(a.dout + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (ES == 2) {
+                s = __builtin_fmaf(__uint_as_float(x[e] << 16), __uint_as_float(g[e] << 16), s);
+                s = __builtin_fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(g[e] & 0xffff0000u), s);
+            } else {
+                s = __builtin_fmaf(__uint_as_float(x[e]), __uint_as_float(g[e]), s);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < L; o *= 2) s += __shfl_xor(s, o);
+    if (p == 0) {
+        const bool none = l == -INFINITY;
+        float* rows = a.rows + (int64_t)bh * 2 * a.Nq;
+        rows[i] = none ? -INFINITY : -l * a.root;
+        rows[a.Nq + i] = none ? 0.f : (a.dlse ? a.dlse[li] - s : -s);
+    }
+}
+
+// The sum of a cut sweep's partials, in order, into the result.
+template <bool BF16>
+__global__ __launch_bounds__(256) void bwd_join_kernel(const float* part, int splits, int64_t elems, void* dst, int accum) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= elems) return;
+    f32x4 v = *(const f32x4*)(part + i);
+    for (int s = 1; s < splits; ++s) v += *(const f32x4*)(part + (int64_t)s * elems + i);
+    if (accum) {
+        f32x4* p = (f32x4*)((float*)dst + i);
+        *p = *p + v;
+    } else if (BF16) {
+        *(u32x2*)((uint16_t*)dst + i) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    } else {
+        *(f32x4*)((float*)dst + i) = v;
+    }
+}
+
+template <int D>
+hipError_t launch_rows(const AttnBwdParams& p, const RowsArgs& a0, hipStream_t s) {
+    RowsArgs a = a0;
+    const int es = p.bf16 ? 2 : 4, ch = D * es / 16;
+    const int R = 256 / (ch <= 8 ? 8 : ch <= 16 ? 16 : 32);
+    a.blocks = (p.Nq + R - 1) / R;
+    const dim3 grid((unsigned)((int64_t)p.B * p.H * a.blocks)), block(256);
+    if (p.bf16) hipLaunchKernelGGL((bwd_rows_kernel<D, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((bwd_rows_kernel<D, 4>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_sweep(BwdArgs a, bool kv, hipStream_t s) {
+    const dim3 grid((unsigned)((int64_t)a.B * a.H * a.r_tiles * a.splits)), block(256);
+    if (kv) hipLaunchKernelGGL((attn_bwd_kernel<D, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_bwd_kernel<D, false>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_bwd_join(const float* part, int splits, int64_t elems, void* dst, int accum, int bf16, hipStream_t s) {
+    const dim3 grid((unsigned)((elems / 4 + 255) / 256)), block(256);
+    if (bf16) hipLaunchKernelGGL(bwd_join_kernel<true>, grid, block, 0, s, part, splits, elems, dst, accum);
+    else hipLaunchKernelGGL(bwd_join_kernel<false>, grid, block, 0, s, part, splits, elems, dst, accum);
+    return hipGetLastError();
+}
+
+hipError_t launch_bwd_rows(const AttnBwdParams& p, hipStream_t s) {
+    RowsArgs a{};
+    a.out = (const char*)p.out, a.dout = (const char*)p.dout, a.lse = p.lse, a.dlse = p.dlse, a.rows = p.rows;
+    a.H = p.H, a.Nq = p.Nq, a.root = sqrtf((float)p.D);
+    if (p.D == 64) return launch_rows<64>(p, a, s);
+    if (p.D == 72) return launch_rows<72>(p, a, s);
+    return launch_rows<128>(p, a, s);
+}
+
+hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, bool kv, hipStream_t s) {
+    BwdArgs a{};
+    a.r1 = (const uint16_t*)(kv ? p.k : p.q);
+    a.r2 = (const uint16_t*)(kv ? p.v : p.dout);
+    a.t1 = (const uint16_t*)(kv ? p.q : p.k);
+    a.t2 = (const uint16_t*)(kv ? p.dout : p.v);
+    a.rows = p.rows;
+    a.o1 = p.dv;
+    a.o2 = kv ? p.dk : p.dq;
+    a.B = p.B, a.H = p.H;
+    a.Nr = kv ? p.Nk : p.Nq, a.Nt = kv ? p.Nq : p.Nk;
+    a.r_tiles = (a.Nr + kRows - 1) / kRows;
+    a.splits = kv ? p.kv_splits : p.q_splits;
+    a.accum = kv ? p.accum_kv : p.accum_q;
+    a.part = p.part;
+    a.part_elems = (int64_t)p.B * a.Nr * p.H * p.D;
+    a.scale = 1.f / sqrtf((float)p.D);
+    a.c2 = a.scale * 1.4426950408889634f;
+    if (p.D == 64) return launch_sweep<64>(a, kv, s);
+    if (p.D == 72) return launch_sweep<72>(a, kv, s);
+    return launch_sweep<128>(a, kv, s);
+}
+
+}  // namespace xdit

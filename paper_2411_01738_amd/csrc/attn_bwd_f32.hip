@@ -1,0 +1,230 @@
+// Gradients of float32 attention: the formulas and sweeps of attn_bwd.hip with
+// float32 products throughout, on v_mfma_f32_32x32x2_f32.
+//
+// What bounds it: the float32 matrix rate, 64 operations per clock and SIMD.
+//
+// One workgroup = 128 resident rows, 4 waves of 32; tiles of 32 streamed rows
+// come straight into LDS, two stages.  X = T1 R1^T and Y = T2 R2^T take both
+// operands' dims in the order hf * d/2 + m, so one 16-byte read feeds four
+// products; in A^T += T^T W the accumulator registers of P and dS are the
+// operand as they stand (rows 8g + i and 8g + 4 + i in the two halves), and T
+// is read by columns, 4 bytes a lane.  d = 72: the third block of 32 dims is
+// padded (its lanes past d read the last dim and are not stored).
+#include "kernels.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+namespace xdit {
+namespace {
+
+#include "attn_common.h"
+
+struct BwdF32Args {
+    const float* r1;
+    const float* r2;
+    const float* t1;
+    const float* t2;
+    const float* rows;  // per (batch, head): [2][Nq] -l sqrt(d), -D
+    float* o1;
+    float* o2;
+    float* part;
+    int64_t part_elems;
+    int B, H, Nr, Nt, r_tiles, splits;
+    int accum;
+    float c2, scale;
+};
+
+constexpr int kRows = 128, kTile = 32;
+
+template <int D, bool KV>
+__global__ __launch_bounds__(256, (D > 96 ? 1 : 2)) void attn_bwd_f32_kernel(BwdF32Args a) {
+    constexpr int CH = D / 4, ROWB = 4 * D, STAGE = kTile * ROWB, DBLK = (D + 31) / 32, KQ = D / 8;
+    constexpr int DMA = STAGE / 1024, DMA_PER_WAVE = (DMA + 3) / 4;
+    constexpr int ROWBASE = 4 * STAGE;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[ROWBASE + (KV ? 2 * 8 * kTile : 0)];
+    static_assert(STAGE % 1024 == 0, "tiles are whole 64-lane loads");
+    auto swz = [](int r) { return D == 72 ? (r >> 3) & 1 : r & 15; };
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 31, hf = lane >> 5;
+    const int logical = xcd_remap(blockIdx.x, gridDim.x);
+    const int sp = logical % a.splits, pair = logical / a.splits;
+    const int rt = pair % a.r_tiles, bh = pair / a.r_tiles;
+    const int hh = bh % a.H, b = bh / a.H;
+    const uint32_t rowb = (uint32_t)a.H * D * 4, headb = (uint32_t)hh * D * 4;
+    const int64_t rs = (int64_t)a.H * D, headoff = (int64_t)hh * D;
+    const int all_tiles = (a.Nt + kTile - 1) / kTile;
+    const int tb = (int)((int64_t)all_tiles * sp / a.splits);
+    const int ntiles = (int)((int64_t)all_tiles * (sp + 1) / a.splits) - tb;
+    auto rows_rsrc = [&](const float* base, int64_t n, int row0) -> Rsrc {
+        return rsrc(base + ((int64_t)b * n + row0) * rs + headoff, n > row0 ? (uint32_t)(n - row0) * rowb - headb : 0u);
+    };
+
+    // resident operands: dims hf * d/2 + 4j .. of row c
+    const int row = rt * kRows + wave * 32 + c;
+    f32x4 r1[KQ], r2[KQ];
+    {
+        const Rsrc q1 = rows_rsrc(a.r1, a.Nr, rt * kRows), q2 = rows_rsrc(a.r2, a.Nr, rt * kRows);
+#pragma unroll
+        for (int j = 0; j < KQ; ++j) {
+            const uint32_t off = (uint32_t)(wave * 32 + c) * rowb + 2 * D * hf + 16 * j;
+            r1[j] = __builtin_bit_cast(f32x4, bload(q1, off));
+            r2[j] = __builtin_bit_cast(f32x4, bload(q2, off));
+        }
+    }
+    float nl = 0.f, nd = 0.f;
+    if constexpr (!KV) {
+        const float* rows = a.rows + (int64_t)bh * 2 * a.Nr;
+        if (row < a.Nr) {
+            nl = rows[row];
+            nd = rows[a.Nr + row];
+        }
+    }
+    uint32_t dma_off[DMA_PER_WAVE];
+#pragma unroll
+    for (int n = 0; n < DMA_PER_WAVE; ++n) {
+        const int p = 64 * (wave + 4 * n) + lane, r = p / CH;
+        dma_off[n] = (uint32_t)r * rowb + 16 * ((p % CH) ^ swz(r));
+    }
+    auto load_tile = [&](int t, int s) {
+        const int lo = (tb + t) * kTile;
+        const Rsrc q1 = rows_rsrc(a.t1, a.Nt, lo), q2 = rows_rsrc(a.t2, a.Nt, lo);
+#pragma unroll
+        for (int n = 0; n < DMA_PER_WAVE; ++n) {
+            const int ins = wave + 4 * n;
+            if (DMA % 4 == 0 || ins < DMA) {
+                dma16(q1, lds + 2 * s * STAGE + 1024 * ins, dma_off[n]);
+                dma16(q2, lds + (2 * s + 1) * STAGE + 1024 * ins, dma_off[n]);
+            }
+        }
+        if constexpr (KV) {
+            if (wave == 3) {  // 32 values of -l sqrt(d), then 32 of -D
+                const Rsrc qr = rsrc(a.rows + (int64_t)bh * 2 * a.Nt, (uint32_t)a.Nt * 8);
+                const int j = lo + c;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_void*)(lds + ROWBASE + 8 * kTile * s), 4,
+                                                         j < a.Nt ? 4u * (uint32_t)(j + (hf ? a.Nt : 0)) : kOOB, 0, 0, 0);
+            }
+        }
+    };
+
+    f32x16 acc1[KV ? DBLK : 1], acc2[DBLK];
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db) {
+        if constexpr (KV) acc1[db] = f32x16{};
+        acc2[db] = f32x16{};
+    }
+    // A^T += T^T W: lane c is dim 32db + c of rows 8g + 4hf + i
+    auto gather = [&](const unsigned char* t, const float (&w)[16], f32x16* acc) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 8 * (i >> 2) + 4 * hf + (i & 3);
+#pragma unroll
+            for (int db = 0; db < DBLK; ++db) {
+                const int dim = D % 32 != 0 && 32 * db + c >= D ? D - 1 : 32 * db + c;
+                const float x = *(const float*)(t + r * ROWB + 16 * ((dim >> 2) ^ swz(r)) + 4 * (dim & 3));
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[i], acc[db], 0, 0, 0);
+            }
+        }
+    };
+
+    if (ntiles > 0) load_tile(0, 0);
+    for (int t = 0; t < ntiles; ++t) {
+        const int s = t & 1;
+        // tile t has landed in every wave, and every wave is done with tile t - 1
+        wait_vmem<0>();
+        __syncthreads();
+        if (t + 1 < ntiles) load_tile(t + 1, s ^ 1);
+        const unsigned char *p1 = lds + 2 * s * STAGE, *p2 = lds + (2 * s + 1) * STAGE;
+        f32x16 x = {}, y = {};
+#pragma unroll
+        for (int j = 0; j < KQ; ++j) {
+            const int lc = hf * (D / 8) + j;
+            const f32x4 u1 = *(const f32x4*)(p1 + c * ROWB + 16 * (lc ^ swz(c)));
+            const f32x4 u2 = *(const f32x4*)(p2 + c * ROWB + 16 * (lc ^ swz(c)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x = __builtin_amdgcn_mfma_f32_32x32x2f32(u1[e], r1[j][e], x, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_32x32x2f32(u2[e], r2[j][e], y, 0, 0, 0);
+            }
+        }
+        float p[16], z[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 l = {nl, nl, nl, nl}, dd = {nd, nd, nd, nd};
+            if constexpr (KV) {
+                const f32x4* q = (const f32x4*)(lds + ROWBASE + 8 * kTile * s + 32 * g + 16 * hf);
+                l = q[0];
+                dd = q[8];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 4 * g + e;
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c2, l[e] * a.c2));
+                // streamed keys past the end have no probability
+                if (!KV && (tb + t) * kTile + 8 * g + 4 * hf + e >= a.Nt) p[i] = 0.f;
+                z[i] = p[i] * (y[i] + dd[e]);
+            }
+        }
+        if constexpr (KV) gather(p2, p, acc1);
+        gather(p1, z, acc2);
+    }
+
+    if (row >= a.Nr) return;
+    const int64_t at0 = ((int64_t)b * a.Nr + row) * rs + headoff;
+    auto result = [&](float* dst, int64_t part0, const f32x16* acc, float f) {
+#pragma unroll
+        for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int dim = 32 * db + 8 * g + 4 * hf;
+                if (D % 32 != 0 && dim >= D) continue;
+                const f32x4 v = f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]} * f;
+                if (a.splits > 1) {
+                    *(f32x4*)(a.part + part0 + (int64_t)sp * a.part_elems + at0 + dim) = v;
+                } else {
+                    f32x4* o = (f32x4*)(dst + at0 + dim);
+                    *o = a.accum ? *o + v : v;
+                }
+            }
+    };
+    result(a.o2, 0, acc2, a.scale);
+    if constexpr (KV) result(a.o1, a.splits * a.part_elems, acc1, 1.f);
+}
+
+template <int D>
+hipError_t launch_sweep(const BwdF32Args& a, bool kv, hipStream_t s) {
+    const dim3 grid((unsigned)((int64_t)a.B * a.H * a.r_tiles * a.splits)), block(256);
+    if (kv) hipLaunchKernelGGL((attn_bwd_f32_kernel<D, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_bwd_f32_kernel<D, false>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_bwd_f32(const AttnBwdParams& p, bool kv, hipStream_t s) {
+    BwdF32Args a{};
+    a.r1 = (const float*)(kv ? p.k : p.q);
+    a.r2 = (const float*)(kv ? p.v : p.dout);
+    a.t1 = (const float*)(kv ? p.q : p.k);
+    a.t2 = (const float*)(kv ? p.dout : p.v);
+    a.rows = p.rows;
+    a.o1 = (float*)p.dv;
+    a.o2 = (float*)(kv ? p.dk : p.dq);
+    a.B = p.B, a.H = p.H;
+    a.Nr = kv ? p.Nk : p.Nq, a.Nt = kv ? p.Nq : p.Nk;
+    a.r_tiles = (a.Nr + kRows - 1) / kRows;
+    a.splits = kv ? p.kv_splits : p.q_splits;
+    a.accum = kv ? p.accum_kv : p.accum_q;
+    a.part = p.part;
+    a.part_elems = (int64_t)p.B * a.Nr * p.H * p.D;
+    a.scale = 1.f / sqrtf((float)p.D);
+    a.c2 = a.scale * 1.4426950408889634f;
+    if (p.D == 64) return launch_sweep<64>(a, kv, s);
+    if (p.D == 72) return launch_sweep<72>(a, kv, s);
+    return launch_sweep<128>(a, kv, s);
+}
+
+}  // namespace xdit

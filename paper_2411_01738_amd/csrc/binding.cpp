@@ -410,6 +410,29 @@ PyObject* qk_norm_rope_bwd(PyObject* const* a) {
     });
 }
 
+// q, k, v, out, lse, dout, dq, dk, dv, dlse, accum_dq, accum_dkv, workspace
+PyObject* chunk_bwd(PyObject* const* a) {
+    Chunk c;
+    T dout, dq, dk, dv, dlse, ws;
+    c10::DeviceIndex dev;
+    if (!chunk_args(a, true, &c) || !current_device(&dev) || !get(a[5], 4, &dout) || !get(a[6], 4, &dq) ||
+        !get(a[7], 4, &dk) || !get(a[8], 4, &dv) || !get_or_none(a[9], 3, &dlse) || !PyBool_Check(a[10]) ||
+        !PyBool_Check(a[11]) || !get_or_none(a[12], -1, &ws))
+        Py_RETURN_NONE;
+    for (int i : {0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 12})
+        if (a[i] != Py_None && !device_of(a[i], dev)) Py_RETURN_NONE;
+    const bool aq = a[10] == Py_True, ak = a[11] == Py_True;
+    const at::ScalarType t = c.q.dt, tq = aq ? at::kFloat : t, tk = ak ? at::kFloat : t;
+    if (!shape4(dout, t, c.B, c.Nq, c.H, c.d) || !shape4(dq, tq, c.B, c.Nq, c.H, c.d) ||
+        !shape4(dk, tk, c.B, c.Nk, c.H, c.d) || !shape4(dv, tk, c.B, c.Nk, c.H, c.d) || !is_lse(dlse, c.B, c.H, c.Nq))
+        Py_RETURN_NONE;
+    return run([&] {
+        return xdit_chunk_attn_bwd(c.q.p, c.k.p, c.v.p, c.out.p, (const float*)c.lse.p, dout.p, (const float*)dlse.p, dq.p,
+                                   dk.p, dv.p, (aq ? XDIT_ACCUM_DQ : 0) | (ak ? XDIT_ACCUM_DKV : 0), ws.p, ws.bytes, c.B,
+                                   c.Nq, c.Nk, c.H, c.d, c.dt);
+    });
+}
+
 // device, raw_stream: the callables that give torch's current stream
 PyObject* init(PyObject* const* a) {
     Py_INCREF(a[0]);
@@ -423,7 +446,8 @@ PyObject* init(PyObject* const* a) {
 PyMethodDef methods[] = {ENTRY(init, 2),         ENTRY(chunk, 6),       ENTRY(chunk_split, 8),
                          ENTRY(patch, 7),        ENTRY(patch_ranges, 7), ENTRY(patch_split, 9),
                          ENTRY(merge, 5),        ENTRY(update, 5),      ENTRY(rope, 6),
-                         ENTRY(qk_norm_rope, 13), ENTRY(qk_norm_rope_bwd, 18), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(qk_norm_rope, 13), ENTRY(qk_norm_rope_bwd, 18), ENTRY(chunk_bwd, 13),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -100,6 +100,19 @@ struct RopeTableParams {
     int64_t n;
 };
 
+// Gradients of one chunk's attention (O and LSE possibly of more chunks).
+struct AttnBwdParams {
+    const void *q, *k, *v;       // [B, Nq or Nk, H, D]
+    const void *out, *dout;      // [B, Nq, H, D]
+    const float *lse, *dlse;     // [B, H, Nq]; dlse or nullptr
+    void *dq, *dk, *dv;
+    int B, H, Nq, Nk, D, bf16;
+    int accum_q, accum_kv;       // dq; dk and dv: float32 sums to add to
+    int q_splits, kv_splits;     // parts that a sweep is cut into, summed by launch_bwd_join
+    float* rows;                 // workspace: [B * H][2][Nq], filled by launch_bwd_rows
+    float* part;                 // workspace of a cut sweep
+};
+
 constexpr int kMaxPartials = 64;
 constexpr int kPartSlotRows = 128;  // query rows of a partitioned launch's tile
 constexpr int kMaxSweepParts = 17;  // most partition ranges one sweep may meet
@@ -129,6 +142,11 @@ hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t s);
 // (norm_rope_bwd_partials floats).
 hipError_t launch_norm_rope_bwd(const NormRopeParams& p, hipStream_t s);
 int64_t norm_rope_bwd_partials(int64_t rows, int heads0, int heads1, int D, bool bf16);
+hipError_t launch_bwd_rows(const AttnBwdParams& p, hipStream_t s);
+// dk and dv (kv) or dq
+hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, bool kv, hipStream_t s);
+hipError_t launch_attn_bwd_f32(const AttnBwdParams& p, bool kv, hipStream_t s);
+hipError_t launch_bwd_join(const float* part, int splits, int64_t elems, void* dst, int accum, int bf16, hipStream_t s);
 hipError_t launch_rope_table(const RopeTableParams& p, hipStream_t s);
 
 }  // namespace xdit

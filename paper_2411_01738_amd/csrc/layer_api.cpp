@@ -1,6 +1,7 @@
 // C ABI of what surrounds the attention in a layer (declared in
-// include/xdit.h): rotary tables, rotation, and the norms of queries and
-// keys, forward and backward.  Checks first, then one dispatch.
+// include/xdit.h): rotary tables, rotation, the norms of queries and keys,
+// forward and backward, and the attention's gradients.  Checks first, then
+// one dispatch.
 #include "layer_api.h"
 
 #include <algorithm>
@@ -166,6 +167,37 @@ void weight_spans(const xdit_qk& p, Span (&w)[4]) {
     w[1] = {p.wk, p.wk ? n : 0, "wk"};
     w[2] = {p.bq, p.bq ? n : 0, "bq"};
     w[3] = {p.bk, p.bk ? n : 0, "bk"};
+}
+
+// How the gradients' sweeps of a call are cut: few resident tiles (128 rows of
+// one head) over a long other side leave CUs idle.  Parts are whole tiles of
+// the streamed side, at least kBwdPartTiles each.
+constexpr int64_t kBwdRows = 128, kBwdSlots = 512, kBwdPartTiles = 4;
+
+int bwd_splits(int64_t bh, int64_t resident, int64_t streamed, int64_t d) {
+    const int64_t wgs = (resident + kBwdRows - 1) / kBwdRows * bh;
+    const int64_t tiles = (streamed + (d > 96 ? 31 : 63)) / (d > 96 ? 32 : 64);
+    if (wgs <= 0) return 1;
+    int64_t s = std::min<int64_t>(kBwdSlots / wgs, tiles / kBwdPartTiles);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(s, XDIT_MAX_SPLITS));
+}
+
+int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
+
+struct BwdPlan {
+    int q_splits, kv_splits;
+    int64_t rows_bytes, bytes;  // of the workspace: the rows' scalars, then the partials of one sweep
+};
+
+BwdPlan bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t d) {
+    BwdPlan p;
+    p.q_splits = bwd_splits(B * H, Nq, Nk, d);
+    p.kv_splits = bwd_splits(B * H, Nk, Nq, d);
+    p.rows_bytes = align256(8 * B * H * Nq);
+    const int64_t q = p.q_splits > 1 ? 4 * p.q_splits * B * Nq * H * d : 0;
+    const int64_t kv = p.kv_splits > 1 ? 8 * p.kv_splits * B * Nk * H * d : 0;
+    p.bytes = p.rows_bytes + align256(std::max(q, kv));
+    return p;
 }
 
 }  // namespace
@@ -366,6 +398,88 @@ int xdit_qk_norm_rope_bwd(const xdit_qk* p, const void* q, const void* k, const 
     }
     r.part = (float*)workspace;
     return hip_status(xdit::launch_norm_rope_bwd(r, g_stream), fn);
+}
+
+int64_t xdit_chunk_attn_bwd_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads,
+                                            int64_t head_dim, int32_t dtype) {
+    clear_error();
+    const char* fn = "xdit_chunk_attn_bwd_workspace_bytes";
+    if (check_dtype_dim(dtype, head_dim) != XDIT_OK || check_dims(fn, batch, q_len, kv_len, heads) != XDIT_OK) return -1;
+    return bwd_plan(batch, q_len, kv_len, heads, head_dim).bytes;
+}
+
+int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,
+                        const void* dout, const float* dlse, void* dq, void* dk, void* dv, int32_t accum,
+                        void* workspace, int64_t workspace_bytes, int64_t batch, int64_t q_len,
+                        int64_t kv_len, int64_t heads, int64_t head_dim, int32_t dtype) {
+    clear_error();
+    const char* fn = "xdit_chunk_attn_bwd";
+    XDIT_TRY(check_dtype_dim(dtype, head_dim));
+    XDIT_TRY(check_dims(fn, batch, q_len, kv_len, heads));
+    const int es = esize_of(dtype);
+    XDIT_TRY(check_batch_bytes(fn, std::max(q_len, kv_len), heads, head_dim, es));
+    if (accum & ~(XDIT_ACCUM_DQ | XDIT_ACCUM_DKV)) return fail(XDIT_ERR_RANGE, "%s: unknown accum %d", fn, accum);
+    const int eq = accum & XDIT_ACCUM_DQ ? 4 : es, ek = accum & XDIT_ACCUM_DKV ? 4 : es;
+    const int64_t nq = batch * q_len * heads, nk = batch * kv_len * heads;
+    const Span sq{q, nq * head_dim * es, "q"}, sk{k, nk * head_dim * es, "k"}, sv{v, nk * head_dim * es, "v"},
+        so{out, nq * head_dim * es, "out"}, sl{lse, nq * 4, "lse"}, sg{dout, nq * head_dim * es, "dout"},
+        se{dlse, dlse ? nq * 4 : 0, "dlse"};
+    const Span gq{dq, nq * head_dim * eq, "dq"}, gk{dk, nk * head_dim * ek, "dk"}, gv{dv, nk * head_dim * ek, "dv"};
+    for (const Span* s : {&sq, &sk, &sv, &so, &sg, &gq, &gk, &gv}) XDIT_TRY(check_ptr(*s));
+    if (nq > 0 && lse == nullptr) return fail(XDIT_ERR_NULL, "lse is NULL");
+    XDIT_TRY(check_f32(sl));
+    XDIT_TRY(check_f32(se));
+    const BwdPlan plan = bwd_plan(batch, q_len, kv_len, heads, head_dim);
+    if (plan.bytes > 0 && (workspace == nullptr || workspace_bytes < plan.bytes))
+        return fail(XDIT_ERR_RANGE, "%s: workspace of %lld bytes needed", fn, (long long)plan.bytes);
+    if (plan.bytes > 0 && ((uintptr_t)workspace & 255u)) return fail(XDIT_ERR_LAYOUT, "%s: workspace is not 256-byte aligned", fn);
+    const Span sw{workspace, plan.bytes, "workspace"};
+    const Span* outs[] = {&gq, &gk, &gv, &sw};
+    for (int i = 0; i < 4; ++i) {
+        for (const Span* s : {&sq, &sk, &sv, &so, &sl, &sg, &se}) XDIT_TRY(check_no_overlap(*outs[i], *s));
+        for (int j = 0; j < i; ++j) XDIT_TRY(check_no_overlap(*outs[i], *outs[j]));
+    }
+    if (batch == 0 || heads == 0) return XDIT_OK;
+    // a grid holds fewer than 2^32 threads: whole batches at a time
+    const int64_t tiles = std::max((q_len + 15) / 16, (kv_len + kBwdRows - 1) / kBwdRows * plan.kv_splits);
+    const int64_t wgs = heads * std::max<int64_t>(1, std::max(tiles, (q_len + kBwdRows - 1) / kBwdRows * plan.q_splits));
+    const int64_t step = std::max<int64_t>(1, (((int64_t)1 << 24) - 1) / wgs);
+    for (int64_t b0 = 0; b0 < batch; b0 += step) {
+        auto at = [&](const void* p, int64_t rows, int bytes) -> char* {
+            return p ? (char*)const_cast<void*>(p) + b0 * rows * heads * bytes : nullptr;
+        };
+        xdit::AttnBwdParams p{};
+        const int d = (int)head_dim;
+        p.q = at(q, q_len, es * d), p.k = at(k, kv_len, es * d), p.v = at(v, kv_len, es * d);
+        p.out = at(out, q_len, es * d), p.dout = at(dout, q_len, es * d);
+        p.lse = (const float*)at(lse, q_len, 4), p.dlse = (const float*)at(dlse, q_len, 4);
+        p.dq = at(dq, q_len, eq * d), p.dk = at(dk, kv_len, ek * d), p.dv = at(dv, kv_len, ek * d);
+        p.B = (int)std::min(step, batch - b0), p.H = (int)heads, p.Nq = (int)q_len, p.Nk = (int)kv_len, p.D = d;
+        p.bf16 = dtype == XDIT_BF16;
+        p.accum_q = (accum & XDIT_ACCUM_DQ) != 0, p.accum_kv = (accum & XDIT_ACCUM_DKV) != 0;
+        p.q_splits = plan.q_splits, p.kv_splits = plan.kv_splits;
+        p.rows = (float*)workspace;
+        p.part = (float*)((char*)workspace + plan.rows_bytes);
+        const auto sweep = p.bf16 ? xdit::launch_attn_bwd_bf16 : xdit::launch_attn_bwd_f32;
+        if (q_len > 0) {
+            XDIT_TRY(hip_status(xdit::launch_bwd_rows(p, g_stream), fn));
+            XDIT_TRY(hip_status(sweep(p, false, g_stream), fn));
+            const int64_t n = (int64_t)p.B * q_len * heads * d;
+            if (p.q_splits > 1)
+                XDIT_TRY(hip_status(xdit::launch_bwd_join(p.part, p.q_splits, n, p.dq, p.accum_q, p.bf16, g_stream), fn));
+        }
+        if (kv_len > 0) {
+            XDIT_TRY(hip_status(sweep(p, true, g_stream), fn));
+            const int64_t n = (int64_t)p.B * kv_len * heads * d;
+            if (p.kv_splits > 1) {
+                XDIT_TRY(hip_status(xdit::launch_bwd_join(p.part, p.kv_splits, n, p.dk, p.accum_kv, p.bf16, g_stream), fn));
+                XDIT_TRY(hip_status(xdit::launch_bwd_join(p.part + p.kv_splits * n, p.kv_splits, n, p.dv, p.accum_kv, p.bf16,
+                                                          g_stream),
+                                    fn));
+            }
+        }
+    }
+    return XDIT_OK;
 }
 
 }  // extern "C"

@@ -95,3 +95,56 @@ def sums_scale(x, g, norm, eps):
     axes = tuple(range(x.ndim - 1))
     big = 2 * np.abs(g).max(-1, keepdims=True)
     return (big * (np.abs(n) + 2 * np.abs(x).max(-1, keepdims=True) * F32)).sum(axes), (big + 0 * n).sum(axes)
+
+
+# -- the attention's gradients --------------------------------------------------
+def attention(q, k, v):
+    """out [B, Nq, H, d] and lse [B, H, Nq] of full attention."""
+    qh, kh, vh = (np.moveaxis(x, 2, 1) for x in (q, k, v))
+    s = qh @ np.swapaxes(kh, 2, 3) / math.sqrt(q.shape[-1])
+    if s.shape[-1] == 0:
+        return np.zeros_like(q), np.full(s.shape[:3], -np.inf)
+    m = s.max(-1, keepdims=True)
+    p = np.exp(s - m)
+    t = p.sum(-1, keepdims=True)
+    return np.moveaxis(p / t @ vh, 1, 2), (m + np.log(t))[..., 0]
+
+
+def attention_bwd(q, k, v, out, lse, dout, dlse=None, dtype="bf16"):
+    """{name: (gradient, worst error, error's deviation)} of dq, dk, dv.
+
+    The worst error counts, for every term of a gradient's sum, half a step of P
+    or dS where they are rounded to the operand type, the float32 error of the
+    exponent (a product of d + 4 roundings of the dot product and of
+    lse * sqrt(d)) and of dout . v - D, one rounding for every addition of the
+    sum, and half a step of the result.  The deviation takes the operands'
+    roundings as independent (their squares add) and the rest as they are."""
+    qh, kh, vh, oh, gh = (np.moveaxis(np.asarray(x, np.float64), 2, 1) for x in (q, k, v, out, dout))
+    d = q.shape[-1]
+    scale = 1 / math.sqrt(d)
+    T = lambda x: np.swapaxes(x, 2, 3)
+    none = np.isneginf(lse)
+    lf = np.where(none, 0.0, lse)[..., None]
+    alive = ~none[..., None]
+    s = qh @ T(kh) * scale
+    P = np.where(alive, np.exp(np.where(alive, s - lf, 0.0)), 0.0)
+    oh = np.where(alive, oh, 0.0)
+    D = (gh * oh).sum(-1, keepdims=True) - (0.0 if dlse is None else np.where(alive, dlse[..., None], 0.0))
+    gv = gh @ T(vh)
+    S = P * (gv - D)
+    op = HALF[dtype] if dtype == "bf16" else 0.0   # rounding of P and dS as operands
+    steps = (d + 8) * F32
+    eP = steps * (scale * (np.abs(qh) @ T(np.abs(kh))) + np.abs(lf)) + 4 * F32
+    eS = P * (steps * (np.abs(gh) @ T(np.abs(vh)) + (np.abs(gh) * np.abs(oh)).sum(-1, keepdims=True)
+                       + (0.0 if dlse is None else np.abs(dlse[..., None])))) + np.abs(S) * (eP + 4 * F32)
+    eS = np.where(alive, eS, 0.0)
+    back = lambda x: np.moveaxis(x, 1, 2)
+    res = {}
+    for name, W, E, X, f, n in (("dq", S, eS, kh, scale, k.shape[1]), ("dk", T(S), T(eS), qh, scale, q.shape[1]),
+                                ("dv", T(P), T(P * eP), gh, 1.0, q.shape[1])):
+        want = W @ X * f
+        small = (E @ np.abs(X) + (n + 20) * F32 * (np.abs(W) @ np.abs(X))) * f
+        worst = small + op * (np.abs(W) @ np.abs(X)) * f + HALF[dtype] * np.abs(want) * 1.01
+        dev = small + op * np.sqrt((W * W) @ (X * X)) * f + HALF[dtype] * np.abs(want)
+        res[name] = tuple(back(x) for x in (want, worst, dev))
+    return res

@@ -66,3 +66,32 @@ def test_table_facts():
     f2 = np.arctan2(*ref.table(one, [8], 100.0, "ramp", 3.0, orig_len=100.0, fast=10.0, slow=1.0)[::-1])
     turns = 100.0 * f0 / (2 * np.pi)
     assert np.allclose(f2[turns >= 10], f0[turns >= 10]) and np.allclose(f2[turns <= 1], f0[turns <= 1] / 3)
+
+
+def test_attention_gradients_by_differences():
+    """Of the outputs and of the log-sum-exp, and of a sequence in two chunks."""
+    rng = np.random.default_rng(6)
+    B, nq, nk, H, d = 1, 3, 5, 2, 8
+    q, k, v = rng.standard_normal((B, nq, H, d)), rng.standard_normal((B, nk, H, d)), rng.standard_normal((B, nk, H, d))
+    g, e = rng.standard_normal((B, nq, H, d)), rng.standard_normal((B, H, nq))
+
+    def loss(q, k, v):
+        o, l = ref.attention(q, k, v)
+        return (o * g).sum() + (l * e).sum()
+
+    out, lse = ref.attention(q, k, v)
+    got = ref.attention_bwd(q, k, v, out, lse, g, e)
+    h = 1e-6
+    for x, name, at in ((q, "dq", 0), (k, "dk", 1), (v, "dv", 2)):
+        for _ in range(12):
+            i = tuple(rng.integers(0, n) for n in x.shape)
+            step = np.zeros_like(x)
+            step[i] = h
+            up, dn = ([*(y + (s * step if j == at else 0) for j, y in enumerate((q, k, v)))] for s in (1, -1))
+            assert abs((loss(*up) - loss(*dn)) / (2 * h) - got[name][0][i]) < 1e-7, name
+    # chunks with the whole sequence's out and lse: parts of dq add up, dk and dv are the chunks'
+    whole = ref.attention_bwd(q, k, v, out, lse, g)
+    parts = [ref.attention_bwd(q, k[:, a:b], v[:, a:b], out, lse, g) for a, b in ((0, 2), (2, 5))]
+    assert np.allclose(sum(p["dq"][0] for p in parts), whole["dq"][0])
+    for n in ("dk", "dv"):
+        assert np.allclose(np.concatenate([p[n][0] for p in parts], 1), whole[n][0])
