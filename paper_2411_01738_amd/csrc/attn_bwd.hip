@@ -184,31 +184,32 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
         else wait_vmem<N * LOADS>();
     };
 
-    // LDS addresses of this lane's operand reads in stage 0 (T1's region)
-    uint32_t kaddr[KSTEPS];
-#pragma unroll
-    for (int kk = 0; kk < KSTEPS; ++kk) {
-        // a chunk past d meets zeros of the resident operand: any finite values do
-        const int r = krow<C::PERM>(c), lc = 2 * kk + hf < C::CH ? 2 * kk + hf : C::CH - 1;
-        kaddr[kk] = lds_u32 + r * C::ROWB + 16 * (lc ^ C::swz(r));
-    }
+    // LDS addresses of this lane's operand reads in stage 0.  Swizzled rows
+    // start at multiples of their own size, so chunks 2kk away are the first
+    // one's address with 32kk exclusive-ored in (dims 32db away: 64db); rows
+    // of d = 72 take them as offsets.
     const int gi = lane & 15, grp = lane >> 4;
-    constexpr int NE = C::SWIZZLED ? 2 : 1, NDB = C::SWIZZLED ? DBLK : 1;
-    uint32_t vaddr[NDB][NE];
+    uint32_t k0, kpad = 0, v0[2], taddr = 0;
+    {
+        const int r = krow<C::PERM>(c);
+        k0 = lds_u32 + r * C::ROWB + 16 * (hf ^ C::swz(r));
+        // the chunk past d of the last k-step meets zeros of the resident
+        // operand: any finite values do (the last chunk's)
+        if constexpr (C::CH % 2 != 0) kpad = lds_u32 + r * C::ROWB + 16 * (C::CH - 1);
+    }
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int e = 0; e < NE; ++e) {
-            const int dim = 32 * db + 16 * (grp & 1) + 4 * (gi & 3);
-            const int r = krow<C::PERM>(4 * hf + (gi >> 2)) + C::E_ROWS * e;
-            vaddr[db][e] = lds_u32 + r * C::ROWB + 16 * ((dim >> 3) ^ C::swz(r)) + 2 * (dim & 7);
-        }
+    for (int e = 0; e < 2; ++e) {
+        const int dim = 16 * (grp & 1) + 4 * (gi & 3);
+        const int r = krow<C::PERM>(4 * hf + (gi >> 2)) + C::E_ROWS * e;
+        v0[e] = lds_u32 + r * C::ROWB + 16 * ((dim >> 3) ^ C::swz(r)) + 2 * (dim & 7);
+    }
     // tail (d = 72): group g reads dims 64..71 of the rows of k-step g & 1, half g >> 1
-    uint32_t taddr = 0;
     if constexpr (C::TAIL) {
         const int r = krow<C::PERM>(4 * (grp >> 1) + (gi >> 2)) + 16 * (grp & 1);
         taddr = lds_u32 + r * C::ROWB + 2 * (32 * DBLK + 4 * (gi & 1));
     }
+    uint32_t ra = lds_u32 + C::ROWBASE + 16 * hf;  // the rows' scalars
+    constexpr int T2OFF = C::T2BASE;
 
     f32x16 acc1[KV ? DBLK : 1], acc2[DBLK];
     f32x4 tail1[2] = {}, tail2[2] = {};
@@ -218,94 +219,136 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
         acc2[db] = f32x16{};
     }
 
-    // A^T += T^T W over one 32-row block, W = w[0], w[1] (16 rows each)
-    auto gather = [&](auto off_c, uint32_t so, const bf16x8 (&w)[2], f32x16* acc, f32x4* tail) {
-        constexpr int OFF = decltype(off_c)::value;
-        u32x2 vr[2][DBLK][2], vt[2];
-        static_for<0, 2>([&](auto ksc) {
-            constexpr int ks = decltype(ksc)::value;
-            static_for<0, DBLK>([&](auto dbc) {
-                constexpr int db = decltype(dbc)::value;
-                if constexpr (C::SWIZZLED) {
-                    vr[ks][db][0] = tr_read<OFF + 16 * ks * C::ROWB>(vaddr[db][0] + so);
-                    vr[ks][db][1] = tr_read<OFF + 16 * ks * C::ROWB>(vaddr[db][NE - 1] + so);
-                } else {
-                    vr[ks][db][0] = tr_read<OFF + 16 * ks * C::ROWB + 64 * db>(vaddr[0][0] + so);
-                    vr[ks][db][1] = tr_read<OFF + (16 * ks + C::E_ROWS) * C::ROWB + 64 * db>(vaddr[0][0] + so);
-                }
-            });
-        });
-        if constexpr (C::TAIL) {
-            vt[0] = tr_read<OFF>(taddr + so);
-            vt[1] = tr_read<OFF + C::E_ROWS * C::ROWB>(taddr + so);
-        }
-        constexpr int T = C::TAIL ? 2 : 0;
-        static_for<0, 2>([&](auto ksc) {
-            constexpr int ks = decltype(ksc)::value;
-            static_for<0, DBLK>([&](auto dbc) {
-                constexpr int db = decltype(dbc)::value;
-                lds_wait_upto<2 * (DBLK * (2 - ks) - db - 1) + T>(vr[ks][db][0], vr[ks][db][1]);
-                const u32x4 v4 = {vr[ks][db][0][0], vr[ks][db][0][1], vr[ks][db][1][0], vr[ks][db][1][1]};
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v4), w[ks], acc[db], 0, 0, 0);
-            });
-        });
-        if constexpr (C::TAIL) {
-            lds_wait_upto<0>(vt[0], vt[1]);
-            const u32x4 x = __builtin_bit_cast(u32x4, w[0]), y = __builtin_bit_cast(u32x4, w[1]);
-            u32x4 b0, b1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const auto r = __builtin_amdgcn_permlane16_swap(x[i], y[i], false, false);
-                b0[i] = r[0];
-                b1[i] = r[1];
-            }
-            const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{vt[0][0], vt[0][1], vt[1][0], vt[1][1]});
-            tail[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b0), tail[0], 0, 0, 0);
-            tail[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b1), tail[1], 0, 0, 0);
+    // The LDS reads of a block are issued by hand, ahead of their products, in
+    // this order: the rows' scalars (KV), the 2 KSTEPS operands of X and Y, the
+    // transposed operands of the sums.  They complete in issue order, so each
+    // product waits for all but the reads issued after its own.
+    constexpr int OPS = 2 * KSTEPS, PF = KV && D > 96 ? 3 : 4;  // operands of X and Y, and how far ahead
+    constexpr int SUMS = (KV ? 4 : 2) * DBLK, GF = 4;           // products of the sums (full blocks), and how far ahead
+    constexpr int GP = KV && D > 96 ? 2 : GF;                   // of which before P and dS (dK/dV at d = 128: registers are short)
+    u32x4 ring[PF];
+    // operand j of X (even) and Y (odd), block at OFF
+    auto read_op = [&](uint32_t so, auto off_c, auto j_c) {
+        constexpr int OFF = decltype(off_c)::value, j = decltype(j_c)::value, kk = j / 2;
+        constexpr int O = OFF + (j & 1 ? T2OFF : 0);
+        if constexpr (C::SWIZZLED) ring[j % PF] = lds_b128<O>((k0 ^ (32 * kk)) + so);
+        else if constexpr (2 * kk + 1 < C::CH) ring[j % PF] = lds_b128<O + 32 * kk>(k0 + so);
+        else ring[j % PF] = lds_b128<O>(kpad + so);
+    };
+    auto first_ops = [&](uint32_t so, auto off_c) {
+        static_for<0, PF>([&](auto j) { read_op(so, off_c, j); });
+    };
+    u32x2 gr[GF][2], gt[2][2];
+    // transposed operand m: acc1's (T2) blocks, k-step by k-step, then acc2's (T1)
+    auto read_sum = [&](uint32_t so, auto off_c, auto m_c) {
+        constexpr int OFF = decltype(off_c)::value, m = decltype(m_c)::value;
+        constexpr bool second = KV && m < 2 * DBLK;
+        constexpr int ks = m / DBLK % 2, db = m % DBLK;
+        constexpr int O = OFF + (second ? T2OFF : 0) + 16 * ks * C::ROWB;
+        if constexpr (C::SWIZZLED) {
+            gr[m % GF][0] = tr_read<O>((v0[0] ^ (64 * db)) + so);
+            gr[m % GF][1] = tr_read<O>((v0[1] ^ (64 * db)) + so);
+        } else {
+            gr[m % GF][0] = tr_read<O + 64 * db>(v0[0] + so);
+            gr[m % GF][1] = tr_read<O + 64 * db>(v0[1] + so);
         }
     };
+    auto read_tails = [&](uint32_t so, auto off_c) {
+        constexpr int OFF = decltype(off_c)::value;
+        if constexpr (C::TAIL) {
+            if constexpr (KV) {
+                gt[0][0] = tr_read<OFF + T2OFF>(taddr + so);
+                gt[0][1] = tr_read<OFF + T2OFF + C::E_ROWS * C::ROWB>(taddr + so);
+            }
+            gt[1][0] = tr_read<OFF>(taddr + so);
+            gt[1][1] = tr_read<OFF + C::E_ROWS * C::ROWB>(taddr + so);
+        }
+    };
+    // the tail's 16 rows: W of 32 streamed rows regrouped to the 16x16x32 layout
+    auto tail_product = [&](const u32x2 (&t)[2], const bf16x8 (&w)[2], f32x4 (&tail)[2]) {
+        const u32x4 x = __builtin_bit_cast(u32x4, w[0]), y = __builtin_bit_cast(u32x4, w[1]);
+        u32x4 b0, b1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const auto r = __builtin_amdgcn_permlane16_swap(x[i], y[i], false, false);
+            b0[i] = r[0];
+            b1[i] = r[1];
+        }
+        const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{t[0][0], t[0][1], t[1][0], t[1][1]});
+        tail[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b0), tail[0], 0, 0, 0);
+        tail[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b1), tail[1], 0, 0, 0);
+    };
 
-    // tile t in stage s
-    auto block = [&](int t, int s, auto kb_c, auto mask_c) {
+    // Block kb of tile t in stage s, whose first PF operands are in flight.
+    // LASTB: the tile's last block, in whose middle tile t + 1 is awaited and
+    // tile t + NST - 1 asked for; the next block's first operands leave before
+    // its last products.
+    auto block = [&](int t, auto kb_c) {
         constexpr int kb = decltype(kb_c)::value;
-        constexpr uint32_t BO = 32 * kb * C::ROWB;
-        const uint32_t so = (uint32_t)(s * C::REGION);
+        constexpr bool LASTB = kb == NB - 1;
+        using Off = std::integral_constant<int, 32 * kb * C::ROWB>;
+        using Next = std::integral_constant<int, LASTB ? 0 : 32 * (kb + 1) * C::ROWB>;
+        const uint32_t so = (uint32_t)(t % NST) * C::REGION;
+        const uint32_t sn = LASTB ? (uint32_t)((t + 1) % NST) * C::REGION : so;
+        if constexpr (KV && D > 96) asm volatile("" : "+v"(k0), "+v"(v0[0]), "+v"(v0[1]));  // addresses derived anew: registers are short
         f32x16 x = {}, y = {};
         if constexpr (KV) {
-            const uint32_t ra = lds_u32 + C::ROWBASE + (uint32_t)(s * C::ROWREGION) + 256 * kb + 16 * hf;
+            constexpr int O = 256 * kb;
+            const uint32_t rs_ = ra + (uint32_t)(t % NST) * C::ROWREGION;
+            u32x4 xi[4], yi[4];
+            static_for<0, 4>([&](auto g_c) {
+                constexpr int g = decltype(g_c)::value;
+                xi[g] = lds_b128<O + 32 * g>(rs_);
+                yi[g] = lds_b128<O + 128 + 32 * g>(rs_);
+            });
+            lds_wait_upto<0>();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 xi = lds_ld<f32x4>(ra + 32 * g), yi = lds_ld<f32x4>(ra + 128 + 32 * g);
+                asm volatile("" : "+v"(xi[g]), "+v"(yi[g]));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[4 * g + i] = xi[i], y[4 * g + i] = yi[i];
+                for (int i = 0; i < 4; ++i) {
+                    x[4 * g + i] = __uint_as_float(xi[g][i]);
+                    y[4 * g + i] = __uint_as_float(yi[g][i]);
+                }
             }
         }
-#pragma unroll
-        for (int kk = 0; kk < KSTEPS; ++kk) {
-            const bf16x8 k1 = lds_ld<bf16x8>(kaddr[kk] + so + BO);
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, r1[kk], x, 0, 0, 0);
-            const bf16x8 k2 = lds_ld<bf16x8>(kaddr[kk] + so + BO + C::T2BASE);
-            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k2, r2[kk], y, 0, 0, 0);
+        static_for<0, OPS>([&](auto j_c) {
+            constexpr int j = decltype(j_c)::value;
+            lgkm_wait_v4<(OPS - 1 - j < PF - 1 ? OPS - 1 - j : PF - 1)>(ring[j % PF]);
+            const bf16x8 op = __builtin_bit_cast(bf16x8, ring[j % PF]);
+            if constexpr (j & 1) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, r2[j / 2], y, 0, 0, 0);
+            else x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, r1[j / 2], x, 0, 0, 0);
+            if constexpr (j + PF < OPS) read_op(so, Off{}, std::integral_constant<int, j + PF>{});
+        });
+        static_for<0, GP>([&](auto m) { read_sum(so, Off{}, m); });
+        if constexpr (LASTB) {
+            // tile t + 1 has landed in every wave (tile t + 2 may be in flight), and
+            // every wave is done with tile t - 1, whose stage takes tile t + NST - 1
+            wait_tiles(std::integral_constant<int, NST - 3>{});
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            load_tile(t + NST - 1, (t + NST - 1) % NST);
         }
         bf16x8 pb[2], zb[2];
+        const bool ragged = !KV && (tb + t + 1) * BN > a.Nt;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             float p[8], z[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int i = 8 * ks + e;
-                if constexpr (KV) {
-                    p[e] = __builtin_amdgcn_exp2f(x[i] * a.c2);
-                    z[e] = p[e] * y[i];
-                } else {
-                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c2, nl));
-                    if constexpr (decltype(mask_c)::value) {
-                        const int j = (tb + t) * BN + 32 * kb + krow<C::PERM>(8 * (i >> 2) + 4 * hf + (i & 3));
-                        if (j >= a.Nt) p[e] = 0.f;
-                    }
-                    z[e] = p[e] * (y[i] + nd);
-                }
+                p[e] = __builtin_amdgcn_exp2f(KV ? x[i] * a.c2 : __builtin_fmaf(x[i], a.c2, nl));
             }
+            if constexpr (!KV)
+                if (ragged)  // streamed keys past the end have no probability
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int i = 8 * ks + e;
+                        if ((tb + t) * BN + 32 * kb + krow<C::PERM>(8 * (i >> 2) + 4 * hf + (i & 3)) >= a.Nt) p[e] = 0.f;
+                    }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = p[e] * (KV ? y[8 * ks + e] : y[8 * ks + e] + nd);
             u32x4 pw, zw;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -315,15 +358,32 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
             if constexpr (KV) pb[ks] = __builtin_bit_cast(bf16x8, pw);
             zb[ks] = __builtin_bit_cast(bf16x8, zw);
         }
-        // d = 72: T2's regions end past a 16-bit offset, so its base is added
-        if constexpr (KV) gather(std::integral_constant<int, (int)BO>{}, so + C::T2BASE, pb, acc1, tail1);
-        gather(std::integral_constant<int, (int)BO>{}, so, zb, acc2, tail2);
+        static_for<GP, GF>([&](auto m) { read_sum(so, Off{}, m); });
+        static_for<0, SUMS>([&](auto m_c) {
+            constexpr int m = decltype(m_c)::value;
+            constexpr bool second = KV && m < 2 * DBLK;
+            constexpr int ks = m / DBLK % 2, db = m % DBLK;
+            constexpr int LEFT = SUMS - GF;  // from here on no more reads are issued, then the tails' and the next operands
+            if constexpr (m == LEFT) read_tails(so, Off{});
+            constexpr int TAILS = C::TAIL ? (KV ? 4 : 2) : 0;
+            if constexpr (m < LEFT) {
+                lds_wait_upto<2 * (GF - 1)>(gr[m % GF][0], gr[m % GF][1]);
+            } else {
+                lds_wait_upto<2 * (SUMS - 1 - m) + TAILS + PF * (m > LEFT)>(gr[m % GF][0], gr[m % GF][1]);
+                if constexpr (m == LEFT) first_ops(sn, Next{});
+            }
+            const bf16x8 va =
+                __builtin_bit_cast(bf16x8, u32x4{gr[m % GF][0][0], gr[m % GF][0][1], gr[m % GF][1][0], gr[m % GF][1][1]});
+            if constexpr (second) acc1[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[ks], acc1[db], 0, 0, 0);
+            else acc2[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, zb[ks], acc2[db], 0, 0, 0);
+            if constexpr (m + GF < SUMS) read_sum(so, Off{}, std::integral_constant<int, m + GF>{});
+        });
+        if constexpr (C::TAIL) {
+            lds_wait_upto<PF>(gt[0][0], gt[0][1], gt[1][0], gt[1][1]);
+            if constexpr (KV) tail_product(gt[0], pb, tail1);
+            tail_product(gt[1], zb, tail2);
+        }
     };
-    auto tile = [&](int t, auto mask_c) {
-        const int s = t % NST;
-        static_for<0, NB>([&](auto kb_c) { block(t, s, kb_c, mask_c); });
-    };
-
     if (ntiles > 0) {
         // the first NST-1 tiles load whether or not there are that many (past
         // the end they read zeros, into stages nobody reads)
@@ -332,18 +392,18 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
 #pragma unroll
         for (int kk = 0; kk < KSTEPS; ++kk) asm volatile("" : "+v"(r1[kk]), "+v"(r2[kk]));
         asm volatile("" : "+v"(nl), "+v"(nd));
-        for (int t = 0; t < ntiles; ++t) {
-            // tile t has landed (two younger may be in flight) in every wave, and
-            // every wave is done with tile t - 1, whose stage takes tile t + NST - 1
-            wait_tiles(std::integral_constant<int, NST - 2>{});
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            load_tile(t + NST - 1, (t + NST - 1) % NST);
-            if (!KV && (tb + t + 1) * BN > a.Nt) tile(t, std::true_type{});
-            else tile(t, std::false_type{});
-        }
+        wait_tiles(std::integral_constant<int, NST - 2>{});
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        first_ops(0, std::integral_constant<int, 0>{});
+        for (int t = 0; t < ntiles; ++t)
+            static_for<0, NB>([&](auto kb_c) { block(t, kb_c); });
     }
+    // the last block's look-ahead reads and the tiles past the end
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < PF; ++j) asm volatile("" : "+v"(ring[j]));
     wait_vmem<0>();
 
     // Results: lane c holds resident row 32 wave + c, dims 32db + 8g + 4hf + i;
