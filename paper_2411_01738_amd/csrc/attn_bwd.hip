@@ -88,16 +88,15 @@ struct BCfg {
     static_assert(REGION % 1024 == 0 && LDS_BYTES <= kLdsBytes / 2, "two workgroups per CU");
 };
 
+// Workgroup `logical` of the dK/dV sweep (KV) or the dQ sweep.
 template <int D, bool KV>
-__global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
+__device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int logical) {
     using C = BCfg<D, KV>;
     constexpr int NST = C::NST, NB = C::NB, BN = C::BN, KSTEPS = C::KSTEPS, DBLK = C::DBLK, NW = C::NW;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS_BYTES];
 
     const int tid = threadIdx.x;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, hf = lane >> 5;
-    const int logical = xcd_remap(blockIdx.x, gridDim.x);
     const int sp = logical % a.splits, pair = logical / a.splits;
     const int rt = pair % a.r_tiles, bh = pair / a.r_tiles;
     const int hh = bh % a.H, b = bh / a.H;
@@ -223,45 +222,61 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
     // this order: the rows' scalars (KV), the 2 KSTEPS operands of X and Y, the
     // transposed operands of the sums.  They complete in issue order, so each
     // product waits for all but the reads issued after its own.
-    constexpr int OPS = 2 * KSTEPS, PF = KV && D > 96 ? 3 : 4;  // operands of X and Y, and how far ahead
-    constexpr int SUMS = (KV ? 4 : 2) * DBLK, GF = 4;           // products of the sums (full blocks), and how far ahead
-    constexpr int GP = KV && D > 96 ? 2 : GF;                   // of which before P and dS (dK/dV at d = 128: registers are short)
+    constexpr int OPS = 2 * KSTEPS, PF = 4;            // operands of X and Y, and how far ahead
+    constexpr int SUMS = (KV ? 4 : 2) * DBLK, GF = 4;  // products of the sums (full blocks), and how far ahead
+    constexpr int GP = KV && D > 96 ? 3 : GF;          // of which before P and dS (dK/dV at d = 128: registers are short)
     u32x4 ring[PF];
+    // Addresses of the current stage: a register per operand where there are
+    // few (one addition each per tile), otherwise derived at each read.
+    constexpr bool HOLD = C::SWIZZLED && D <= 96;
+    uint32_t ka[HOLD ? KSTEPS : 1], va0[HOLD ? DBLK : 1][2], kp = 0, ta = 0;
+    auto k_stage = [&](uint32_t so) {
+#pragma unroll
+        for (int kk = 0; kk < (HOLD ? KSTEPS : 1); ++kk) ka[kk] = (k0 ^ (32 * kk)) + so;
+        if constexpr (!C::SWIZZLED) kp = kpad + so;
+    };
+    auto v_stage = [&](uint32_t so) {
+#pragma unroll
+        for (int db = 0; db < (HOLD ? DBLK : 1); ++db)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) va0[db][e] = (v0[e] ^ (64 * db)) + so;
+        if constexpr (C::TAIL) ta = taddr + so;
+    };
     // operand j of X (even) and Y (odd), block at OFF
-    auto read_op = [&](uint32_t so, auto off_c, auto j_c) {
+    auto read_op = [&](auto off_c, auto j_c) {
         constexpr int OFF = decltype(off_c)::value, j = decltype(j_c)::value, kk = j / 2;
         constexpr int O = OFF + (j & 1 ? T2OFF : 0);
-        if constexpr (C::SWIZZLED) ring[j % PF] = lds_b128<O>((k0 ^ (32 * kk)) + so);
-        else if constexpr (2 * kk + 1 < C::CH) ring[j % PF] = lds_b128<O + 32 * kk>(k0 + so);
-        else ring[j % PF] = lds_b128<O>(kpad + so);
+        if constexpr (HOLD) ring[j % PF] = lds_b128<O>(ka[kk]);
+        else if constexpr (C::SWIZZLED) ring[j % PF] = lds_b128<O>(ka[0] ^ (32 * kk));
+        else if constexpr (2 * kk + 1 < C::CH) ring[j % PF] = lds_b128<O + 32 * kk>(ka[0]);
+        else ring[j % PF] = lds_b128<O>(kp);
     };
-    auto first_ops = [&](uint32_t so, auto off_c) {
-        static_for<0, PF>([&](auto j) { read_op(so, off_c, j); });
+    auto first_ops = [&](auto off_c) {
+        static_for<0, PF>([&](auto j) { read_op(off_c, j); });
     };
     u32x2 gr[GF][2], gt[2][2];
     // transposed operand m: acc1's (T2) blocks, k-step by k-step, then acc2's (T1)
-    auto read_sum = [&](uint32_t so, auto off_c, auto m_c) {
+    auto read_sum = [&](auto off_c, auto m_c) {
         constexpr int OFF = decltype(off_c)::value, m = decltype(m_c)::value;
         constexpr bool second = KV && m < 2 * DBLK;
         constexpr int ks = m / DBLK % 2, db = m % DBLK;
         constexpr int O = OFF + (second ? T2OFF : 0) + 16 * ks * C::ROWB;
-        if constexpr (C::SWIZZLED) {
-            gr[m % GF][0] = tr_read<O>((v0[0] ^ (64 * db)) + so);
-            gr[m % GF][1] = tr_read<O>((v0[1] ^ (64 * db)) + so);
-        } else {
-            gr[m % GF][0] = tr_read<O + 64 * db>(v0[0] + so);
-            gr[m % GF][1] = tr_read<O + 64 * db>(v0[1] + so);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if constexpr (HOLD) gr[m % GF][e] = tr_read<O>(va0[db][e]);
+            else if constexpr (C::SWIZZLED) gr[m % GF][e] = tr_read<O>(va0[0][e] ^ (64 * db));
+            else gr[m % GF][e] = tr_read<O + 64 * db>(va0[0][e]);
         }
     };
-    auto read_tails = [&](uint32_t so, auto off_c) {
+    auto read_tails = [&](auto off_c) {
         constexpr int OFF = decltype(off_c)::value;
         if constexpr (C::TAIL) {
             if constexpr (KV) {
-                gt[0][0] = tr_read<OFF + T2OFF>(taddr + so);
-                gt[0][1] = tr_read<OFF + T2OFF + C::E_ROWS * C::ROWB>(taddr + so);
+                gt[0][0] = tr_read<OFF + T2OFF>(ta);
+                gt[0][1] = tr_read<OFF + T2OFF + C::E_ROWS * C::ROWB>(ta);
             }
-            gt[1][0] = tr_read<OFF>(taddr + so);
-            gt[1][1] = tr_read<OFF + C::E_ROWS * C::ROWB>(taddr + so);
+            gt[1][0] = tr_read<OFF>(ta);
+            gt[1][1] = tr_read<OFF + C::E_ROWS * C::ROWB>(ta);
         }
     };
     // the tail's 16 rows: W of 32 streamed rows regrouped to the 16x16x32 layout
@@ -279,6 +294,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
         tail[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b1), tail[1], 0, 0, 0);
     };
 
+    f32x16 ndv;
     // Block kb of tile t in stage s, whose first PF operands are in flight.
     // LASTB: the tile's last block, in whose middle tile t + 1 is awaited and
     // tile t + NST - 1 asked for; the next block's first operands leave before
@@ -288,10 +304,11 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
         constexpr bool LASTB = kb == NB - 1;
         using Off = std::integral_constant<int, 32 * kb * C::ROWB>;
         using Next = std::integral_constant<int, LASTB ? 0 : 32 * (kb + 1) * C::ROWB>;
-        const uint32_t so = (uint32_t)(t % NST) * C::REGION;
-        const uint32_t sn = LASTB ? (uint32_t)((t + 1) % NST) * C::REGION : so;
-        if constexpr (KV && D > 96) asm volatile("" : "+v"(k0), "+v"(v0[0]), "+v"(v0[1]));  // addresses derived anew: registers are short
-        f32x16 x = {}, y = {};
+        // (opaque: the addresses derived from these are not kept in registers)
+        if constexpr (C::SWIZZLED && !HOLD) asm volatile("" : "+v"(ka[0]));
+        if constexpr (kb == 0) v_stage((uint32_t)(t % NST) * C::REGION);
+        if constexpr (C::SWIZZLED && !HOLD) asm volatile("" : "+v"(va0[0][0]), "+v"(va0[0][1]));
+        f32x16 x = {}, y = KV ? f32x16{} : ndv;
         if constexpr (KV) {
             constexpr int O = 256 * kb;
             const uint32_t rs_ = ra + (uint32_t)(t % NST) * C::ROWREGION;
@@ -318,9 +335,9 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
             const bf16x8 op = __builtin_bit_cast(bf16x8, ring[j % PF]);
             if constexpr (j & 1) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, r2[j / 2], y, 0, 0, 0);
             else x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, r1[j / 2], x, 0, 0, 0);
-            if constexpr (j + PF < OPS) read_op(so, Off{}, std::integral_constant<int, j + PF>{});
+            if constexpr (j + PF < OPS) read_op(Off{}, std::integral_constant<int, j + PF>{});
         });
-        static_for<0, GP>([&](auto m) { read_sum(so, Off{}, m); });
+        static_for<0, GP>([&](auto m) { read_sum(Off{}, m); });
         if constexpr (LASTB) {
             // tile t + 1 has landed in every wave (tile t + 2 may be in flight), and
             // every wave is done with tile t - 1, whose stage takes tile t + NST - 1
@@ -348,7 +365,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
                         if ((tb + t) * BN + 32 * kb + krow<C::PERM>(8 * (i >> 2) + 4 * hf + (i & 3)) >= a.Nt) p[e] = 0.f;
                     }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = p[e] * (KV ? y[8 * ks + e] : y[8 * ks + e] + nd);
+            for (int e = 0; e < 8; ++e) z[e] = p[e] * y[8 * ks + e];
             u32x4 pw, zw;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -358,25 +375,28 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
             if constexpr (KV) pb[ks] = __builtin_bit_cast(bf16x8, pw);
             zb[ks] = __builtin_bit_cast(bf16x8, zw);
         }
-        static_for<GP, GF>([&](auto m) { read_sum(so, Off{}, m); });
+        static_for<GP, GF>([&](auto m) { read_sum(Off{}, m); });
         static_for<0, SUMS>([&](auto m_c) {
             constexpr int m = decltype(m_c)::value;
             constexpr bool second = KV && m < 2 * DBLK;
             constexpr int ks = m / DBLK % 2, db = m % DBLK;
             constexpr int LEFT = SUMS - GF;  // from here on no more reads are issued, then the tails' and the next operands
-            if constexpr (m == LEFT) read_tails(so, Off{});
+            if constexpr (m == LEFT) read_tails(Off{});
             constexpr int TAILS = C::TAIL ? (KV ? 4 : 2) : 0;
             if constexpr (m < LEFT) {
                 lds_wait_upto<2 * (GF - 1)>(gr[m % GF][0], gr[m % GF][1]);
             } else {
                 lds_wait_upto<2 * (SUMS - 1 - m) + TAILS + PF * (m > LEFT)>(gr[m % GF][0], gr[m % GF][1]);
-                if constexpr (m == LEFT) first_ops(sn, Next{});
+                if constexpr (m == LEFT) {
+                    if constexpr (LASTB) k_stage((uint32_t)((t + 1) % NST) * C::REGION);
+                    first_ops(Next{});
+                }
             }
             const bf16x8 va =
                 __builtin_bit_cast(bf16x8, u32x4{gr[m % GF][0][0], gr[m % GF][0][1], gr[m % GF][1][0], gr[m % GF][1][1]});
             if constexpr (second) acc1[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[ks], acc1[db], 0, 0, 0);
             else acc2[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, zb[ks], acc2[db], 0, 0, 0);
-            if constexpr (m + GF < SUMS) read_sum(so, Off{}, std::integral_constant<int, m + GF>{});
+            if constexpr (m + GF < SUMS) read_sum(Off{}, std::integral_constant<int, m + GF>{});
         });
         if constexpr (C::TAIL) {
             lds_wait_upto<PF>(gt[0][0], gt[0][1], gt[1][0], gt[1][1]);
@@ -392,11 +412,19 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
 #pragma unroll
         for (int kk = 0; kk < KSTEPS; ++kk) asm volatile("" : "+v"(r1[kk]), "+v"(r2[kk]));
         asm volatile("" : "+v"(nl), "+v"(nd));
+        // what Y of dQ starts from: -D of the lane's row, a register per value so
+        // that the first product takes it as it stands
+        if constexpr (!KV) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ndv[i] = nd;
+            asm volatile("" : "+v"(ndv));
+        }
         wait_tiles(std::integral_constant<int, NST - 2>{});
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        first_ops(0, std::integral_constant<int, 0>{});
+        k_stage(0);
+        first_ops(std::integral_constant<int, 0>{});
         for (int t = 0; t < ntiles; ++t)
             static_for<0, NB>([&](auto kb_c) { block(t, kb_c); });
     }
@@ -434,6 +462,17 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs a) {
     };
     result(a.o2, 0, acc2, tail2, a.scale);
     if constexpr (KV) result(a.o1, a.splits * a.part_elems, acc1, tail1, 1.f);
+}
+
+// Both sweeps in one launch: they need nothing of each other, and the shorter
+// dQ workgroups fill the CUs that the last dK/dV ones leave.  The first n_kv
+// workgroups are those of dK/dV.
+template <int D>
+__global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs kv, BwdArgs q, int n_kv) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[BCfg<D, true>::LDS_BYTES];
+    const int id = blockIdx.x;
+    if (id < n_kv) sweep<D, true>(kv, lds, xcd_remap(id, n_kv));
+    else sweep<D, false>(q, lds, xcd_remap(id - n_kv, gridDim.x - n_kv));
 }
 
 // Per query row: -l sqrt(d) and -D = e - g . o.  A row whose l is -inf (no
@@ -486,20 +525,29 @@ __global__ __launch_bounds__(256) void bwd_rows_kernel(RowsArgs a) {
     }
 }
 
-// The sum of a cut sweep's partials, in order, into the result.
+// The sums of cut sweeps' partials, in order, into the results (blockIdx.y).
+struct JoinArgs {
+    const float* part[3];
+    void* dst[3];
+    int64_t elems[3];
+    int splits[3], accum[3];
+};
+
 template <bool BF16>
-__global__ __launch_bounds__(256) void bwd_join_kernel(const float* part, int splits, int64_t elems, void* dst, int accum) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= elems) return;
-    f32x4 v = *(const f32x4*)(part + i);
-    for (int s = 1; s < splits; ++s) v += *(const f32x4*)(part + (int64_t)s * elems + i);
-    if (accum) {
-        f32x4* p = (f32x4*)((float*)dst + i);
+__global__ __launch_bounds__(256) void bwd_join_kernel(JoinArgs a) {
+    const int y = blockIdx.y;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = a.elems[y];
+    if (i >= n) return;
+    const float* part = a.part[y] + i;
+    f32x4 v = *(const f32x4*)part;
+    for (int s = 1; s < a.splits[y]; ++s) v += *(const f32x4*)(part + s * n);
+    if (a.accum[y]) {
+        f32x4* p = (f32x4*)((float*)a.dst[y] + i);
         *p = *p + v;
     } else if (BF16) {
-        *(u32x2*)((uint16_t*)dst + i) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        *(u32x2*)((uint16_t*)a.dst[y] + i) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     } else {
-        *(f32x4*)((float*)dst + i) = v;
+        *(f32x4*)((float*)a.dst[y] + i) = v;
     }
 }
 
@@ -515,33 +563,8 @@ hipError_t launch_rows(const AttnBwdParams& p, const RowsArgs& a0, hipStream_t s
     return hipGetLastError();
 }
 
-template <int D>
-hipError_t launch_sweep(BwdArgs a, bool kv, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.B * a.H * a.r_tiles * a.splits)), block(256);
-    if (kv) hipLaunchKernelGGL((attn_bwd_kernel<D, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_bwd_kernel<D, false>), grid, block, 0, s, a);
-    return hipGetLastError();
-}
-
-}  // namespace
-
-hipError_t launch_bwd_join(const float* part, int splits, int64_t elems, void* dst, int accum, int bf16, hipStream_t s) {
-    const dim3 grid((unsigned)((elems / 4 + 255) / 256)), block(256);
-    if (bf16) hipLaunchKernelGGL(bwd_join_kernel<true>, grid, block, 0, s, part, splits, elems, dst, accum);
-    else hipLaunchKernelGGL(bwd_join_kernel<false>, grid, block, 0, s, part, splits, elems, dst, accum);
-    return hipGetLastError();
-}
-
-hipError_t launch_bwd_rows(const AttnBwdParams& p, hipStream_t s) {
-    RowsArgs a{};
-    a.out = (const char*)p.out, a.dout = (const char*)p.dout, a.lse = p.lse, a.dlse = p.dlse, a.rows = p.rows;
-    a.H = p.H, a.Nq = p.Nq, a.root = sqrtf((float)p.D);
-    if (p.D == 64) return launch_rows<64>(p, a, s);
-    if (p.D == 72) return launch_rows<72>(p, a, s);
-    return launch_rows<128>(p, a, s);
-}
-
-hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, bool kv, hipStream_t s) {
+// kv: the dK/dV sweep's arguments, else the dQ sweep's
+BwdArgs sweep_args(const AttnBwdParams& p, bool kv) {
     BwdArgs a{};
     a.r1 = (const uint16_t*)(kv ? p.k : p.q);
     a.r2 = (const uint16_t*)(kv ? p.v : p.dout);
@@ -555,13 +578,62 @@ hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, bool kv, hipStream_t s) 
     a.r_tiles = (a.Nr + kRows - 1) / kRows;
     a.splits = kv ? p.kv_splits : p.q_splits;
     a.accum = kv ? p.accum_kv : p.accum_q;
-    a.part = p.part;
+    a.part = kv ? p.kv_part : p.q_part;
     a.part_elems = (int64_t)p.B * a.Nr * p.H * p.D;
     a.scale = 1.f / sqrtf((float)p.D);
     a.c2 = a.scale * 1.4426950408889634f;
-    if (p.D == 64) return launch_sweep<64>(a, kv, s);
-    if (p.D == 72) return launch_sweep<72>(a, kv, s);
-    return launch_sweep<128>(a, kv, s);
+    return a;
+}
+
+int64_t workgroups(const BwdArgs& a) { return (int64_t)a.B * a.H * a.r_tiles * a.splits; }
+
+template <int D>
+hipError_t launch_sweeps(const BwdArgs& kv, const BwdArgs& q, hipStream_t s) {
+    const int64_t n_kv = workgroups(kv), n = n_kv + workgroups(q);
+    if (n == 0) return hipSuccess;
+    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)n), dim3(256), 0, s, kv, q, (int)n_kv);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_bwd_join(const AttnBwdParams& p, hipStream_t s) {
+    JoinArgs a{};
+    int n = 0;
+    int64_t most = 0;
+    auto add = [&](const float* part, void* dst, int64_t elems, int splits, int accum) {
+        a.part[n] = part, a.dst[n] = dst, a.elems[n] = elems, a.splits[n] = splits, a.accum[n] = accum;
+        if (elems > most) most = elems;
+        ++n;
+    };
+    const int64_t nq = (int64_t)p.B * p.Nq * p.H * p.D, nk = (int64_t)p.B * p.Nk * p.H * p.D;
+    if (p.q_splits > 1) add(p.q_part, p.dq, nq, p.q_splits, p.accum_q);
+    if (p.kv_splits > 1) {
+        add(p.kv_part, p.dk, nk, p.kv_splits, p.accum_kv);
+        add(p.kv_part + p.kv_splits * nk, p.dv, nk, p.kv_splits, p.accum_kv);
+    }
+    if (most == 0) return hipSuccess;
+    const dim3 grid((unsigned)((most / 4 + 255) / 256), (unsigned)n), block(256);
+    if (p.bf16) hipLaunchKernelGGL(bwd_join_kernel<true>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(bwd_join_kernel<false>, grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_bwd_rows(const AttnBwdParams& p, hipStream_t s) {
+    RowsArgs a{};
+    a.out = (const char*)p.out, a.dout = (const char*)p.dout, a.lse = p.lse, a.dlse = p.dlse, a.rows = p.rows;
+    a.H = p.H, a.Nq = p.Nq, a.root = sqrtf((float)p.D);
+    if ((int64_t)p.B * p.H * p.Nq == 0) return hipSuccess;
+    if (p.D == 64) return launch_rows<64>(p, a, s);
+    if (p.D == 72) return launch_rows<72>(p, a, s);
+    return launch_rows<128>(p, a, s);
+}
+
+hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, hipStream_t s) {
+    const BwdArgs kv = sweep_args(p, true), q = sweep_args(p, false);
+    if (p.D == 64) return launch_sweeps<64>(kv, q, s);
+    if (p.D == 72) return launch_sweeps<72>(kv, q, s);
+    return launch_sweeps<128>(kv, q, s);
 }
 
 }  // namespace xdit

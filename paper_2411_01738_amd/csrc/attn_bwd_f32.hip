@@ -38,19 +38,23 @@ struct BwdF32Args {
 
 constexpr int kRows = 128, kTile = 32;
 
+// LDS: two stages of both tiles, then of the rows' scalars
+template <int D>
+constexpr int lds_bytes() {
+    return 4 * kTile * 4 * D + 2 * 8 * kTile;
+}
+
 template <int D, bool KV>
-__global__ __launch_bounds__(256, (D > 96 ? 1 : 2)) void attn_bwd_f32_kernel(BwdF32Args a) {
+__device__ __forceinline__ void sweep(const BwdF32Args& a, unsigned char* lds, int logical) {
     constexpr int CH = D / 4, ROWB = 4 * D, STAGE = kTile * ROWB, DBLK = (D + 31) / 32, KQ = D / 8;
     constexpr int DMA = STAGE / 1024, DMA_PER_WAVE = (DMA + 3) / 4;
     constexpr int ROWBASE = 4 * STAGE;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[ROWBASE + (KV ? 2 * 8 * kTile : 0)];
     static_assert(STAGE % 1024 == 0, "tiles are whole 64-lane loads");
     auto swz = [](int r) { return D == 72 ? (r >> 3) & 1 : r & 15; };
 
     const int tid = threadIdx.x;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, hf = lane >> 5;
-    const int logical = xcd_remap(blockIdx.x, gridDim.x);
     const int sp = logical % a.splits, pair = logical / a.splits;
     const int rt = pair % a.r_tiles, bh = pair / a.r_tiles;
     const int hh = bh % a.H, b = bh / a.H;
@@ -194,17 +198,16 @@ __global__ __launch_bounds__(256, (D > 96 ? 1 : 2)) void attn_bwd_f32_kernel(Bwd
     if constexpr (KV) result(a.o1, a.splits * a.part_elems, acc1, 1.f);
 }
 
+// Both sweeps in one launch, the dK/dV workgroups first.
 template <int D>
-hipError_t launch_sweep(const BwdF32Args& a, bool kv, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.B * a.H * a.r_tiles * a.splits)), block(256);
-    if (kv) hipLaunchKernelGGL((attn_bwd_f32_kernel<D, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_bwd_f32_kernel<D, false>), grid, block, 0, s, a);
-    return hipGetLastError();
+__global__ __launch_bounds__(256, (D > 96 ? 1 : 2)) void attn_bwd_f32_kernel(BwdF32Args kv, BwdF32Args q, int n_kv) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[lds_bytes<D>()];
+    const int id = blockIdx.x;
+    if (id < n_kv) sweep<D, true>(kv, lds, xcd_remap(id, n_kv));
+    else sweep<D, false>(q, lds, xcd_remap(id - n_kv, gridDim.x - n_kv));
 }
 
-}  // namespace
-
-hipError_t launch_attn_bwd_f32(const AttnBwdParams& p, bool kv, hipStream_t s) {
+BwdF32Args sweep_args(const AttnBwdParams& p, bool kv) {
     BwdF32Args a{};
     a.r1 = (const float*)(kv ? p.k : p.q);
     a.r2 = (const float*)(kv ? p.v : p.dout);
@@ -218,13 +221,29 @@ hipError_t launch_attn_bwd_f32(const AttnBwdParams& p, bool kv, hipStream_t s) {
     a.r_tiles = (a.Nr + kRows - 1) / kRows;
     a.splits = kv ? p.kv_splits : p.q_splits;
     a.accum = kv ? p.accum_kv : p.accum_q;
-    a.part = p.part;
+    a.part = kv ? p.kv_part : p.q_part;
     a.part_elems = (int64_t)p.B * a.Nr * p.H * p.D;
     a.scale = 1.f / sqrtf((float)p.D);
     a.c2 = a.scale * 1.4426950408889634f;
-    if (p.D == 64) return launch_sweep<64>(a, kv, s);
-    if (p.D == 72) return launch_sweep<72>(a, kv, s);
-    return launch_sweep<128>(a, kv, s);
+    return a;
+}
+
+template <int D>
+hipError_t launch_sweeps(const BwdF32Args& kv, const BwdF32Args& q, hipStream_t s) {
+    const int64_t n_kv = (int64_t)kv.B * kv.H * kv.r_tiles * kv.splits;
+    const int64_t n = n_kv + (int64_t)q.B * q.H * q.r_tiles * q.splits;
+    if (n == 0) return hipSuccess;
+    hipLaunchKernelGGL(attn_bwd_f32_kernel<D>, dim3((unsigned)n), dim3(256), 0, s, kv, q, (int)n_kv);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_bwd_f32(const AttnBwdParams& p, hipStream_t s) {
+    const BwdF32Args kv = sweep_args(p, true), q = sweep_args(p, false);
+    if (p.D == 64) return launch_sweeps<64>(kv, q, s);
+    if (p.D == 72) return launch_sweeps<72>(kv, q, s);
+    return launch_sweeps<128>(kv, q, s);
 }
 
 }  // namespace xdit

@@ -110,7 +110,7 @@ struct AttnBwdParams {
     int accum_q, accum_kv;       // dq; dk and dv: float32 sums to add to
     int q_splits, kv_splits;     // parts that a sweep is cut into, summed by launch_bwd_join
     float* rows;                 // workspace: [B * H][2][Nq], filled by launch_bwd_rows
-    float* part;                 // workspace of a cut sweep
+    float *q_part, *kv_part;     // workspace of cut sweeps: [splits][B, N, H, D], dk's and then dv's
 };
 
 constexpr int kMaxPartials = 64;
@@ -143,10 +143,11 @@ hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t s);
 hipError_t launch_norm_rope_bwd(const NormRopeParams& p, hipStream_t s);
 int64_t norm_rope_bwd_partials(int64_t rows, int heads0, int heads1, int D, bool bf16);
 hipError_t launch_bwd_rows(const AttnBwdParams& p, hipStream_t s);
-// dk and dv (kv) or dq
-hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, bool kv, hipStream_t s);
-hipError_t launch_attn_bwd_f32(const AttnBwdParams& p, bool kv, hipStream_t s);
-hipError_t launch_bwd_join(const float* part, int splits, int64_t elems, void* dst, int accum, int bf16, hipStream_t s);
+// both sweeps: dq, dk and dv, or the partials of the cut ones
+hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, hipStream_t s);
+hipError_t launch_attn_bwd_f32(const AttnBwdParams& p, hipStream_t s);
+// the sums of the cut sweeps' partials (nothing to do where none is cut)
+hipError_t launch_bwd_join(const AttnBwdParams& p, hipStream_t s);
 hipError_t launch_rope_table(const RopeTableParams& p, hipStream_t s);
 
 }  // namespace xdit

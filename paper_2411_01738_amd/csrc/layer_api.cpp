@@ -186,7 +186,7 @@ int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 
 struct BwdPlan {
     int q_splits, kv_splits;
-    int64_t rows_bytes, bytes;  // of the workspace: the rows' scalars, then the partials of one sweep
+    int64_t rows_bytes, q_bytes, bytes;  // of the workspace: the rows' scalars, then the partials of dq, of dk and dv
 };
 
 BwdPlan bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t d) {
@@ -194,9 +194,8 @@ BwdPlan bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t d) {
     p.q_splits = bwd_splits(B * H, Nq, Nk, d);
     p.kv_splits = bwd_splits(B * H, Nk, Nq, d);
     p.rows_bytes = align256(8 * B * H * Nq);
-    const int64_t q = p.q_splits > 1 ? 4 * p.q_splits * B * Nq * H * d : 0;
-    const int64_t kv = p.kv_splits > 1 ? 8 * p.kv_splits * B * Nk * H * d : 0;
-    p.bytes = p.rows_bytes + align256(std::max(q, kv));
+    p.q_bytes = p.q_splits > 1 ? align256(4 * p.q_splits * B * Nq * H * d) : 0;
+    p.bytes = p.rows_bytes + p.q_bytes + (p.kv_splits > 1 ? align256(8 * p.kv_splits * B * Nk * H * d) : 0);
     return p;
 }
 
@@ -441,8 +440,8 @@ int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void*
     }
     if (batch == 0 || heads == 0) return XDIT_OK;
     // a grid holds fewer than 2^32 threads: whole batches at a time
-    const int64_t tiles = std::max((q_len + 15) / 16, (kv_len + kBwdRows - 1) / kBwdRows * plan.kv_splits);
-    const int64_t wgs = heads * std::max<int64_t>(1, std::max(tiles, (q_len + kBwdRows - 1) / kBwdRows * plan.q_splits));
+    const int64_t sweeps = (kv_len + kBwdRows - 1) / kBwdRows * plan.kv_splits + (q_len + kBwdRows - 1) / kBwdRows * plan.q_splits;
+    const int64_t wgs = heads * std::max<int64_t>(1, std::max((q_len + 7) / 8, sweeps));
     const int64_t step = std::max<int64_t>(1, (((int64_t)1 << 24) - 1) / wgs);
     for (int64_t b0 = 0; b0 < batch; b0 += step) {
         auto at = [&](const void* p, int64_t rows, int bytes) -> char* {
@@ -459,25 +458,11 @@ int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void*
         p.accum_q = (accum & XDIT_ACCUM_DQ) != 0, p.accum_kv = (accum & XDIT_ACCUM_DKV) != 0;
         p.q_splits = plan.q_splits, p.kv_splits = plan.kv_splits;
         p.rows = (float*)workspace;
-        p.part = (float*)((char*)workspace + plan.rows_bytes);
-        const auto sweep = p.bf16 ? xdit::launch_attn_bwd_bf16 : xdit::launch_attn_bwd_f32;
-        if (q_len > 0) {
-            XDIT_TRY(hip_status(xdit::launch_bwd_rows(p, g_stream), fn));
-            XDIT_TRY(hip_status(sweep(p, false, g_stream), fn));
-            const int64_t n = (int64_t)p.B * q_len * heads * d;
-            if (p.q_splits > 1)
-                XDIT_TRY(hip_status(xdit::launch_bwd_join(p.part, p.q_splits, n, p.dq, p.accum_q, p.bf16, g_stream), fn));
-        }
-        if (kv_len > 0) {
-            XDIT_TRY(hip_status(sweep(p, true, g_stream), fn));
-            const int64_t n = (int64_t)p.B * kv_len * heads * d;
-            if (p.kv_splits > 1) {
-                XDIT_TRY(hip_status(xdit::launch_bwd_join(p.part, p.kv_splits, n, p.dk, p.accum_kv, p.bf16, g_stream), fn));
-                XDIT_TRY(hip_status(xdit::launch_bwd_join(p.part + p.kv_splits * n, p.kv_splits, n, p.dv, p.accum_kv, p.bf16,
-                                                          g_stream),
-                                    fn));
-            }
-        }
+        p.q_part = (float*)((char*)workspace + plan.rows_bytes);
+        p.kv_part = (float*)((char*)workspace + plan.rows_bytes + plan.q_bytes);
+        XDIT_TRY(hip_status(xdit::launch_bwd_rows(p, g_stream), fn));
+        XDIT_TRY(hip_status((p.bf16 ? xdit::launch_attn_bwd_bf16 : xdit::launch_attn_bwd_f32)(p, g_stream), fn));
+        XDIT_TRY(hip_status(xdit::launch_bwd_join(p, g_stream), fn));
     }
     return XDIT_OK;
 }
