@@ -33,10 +33,7 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # ILP strategy, which interleaves their matrix products and softmax VALU work
 # better than the default occupancy strategy (measured 1-3 % faster at head
 # dims 64, 72 and 128, same register counts within a few).
-EXTRA = {"attn_bf16.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"],
-         # the gradients order their LDS reads by hand; this strategy keeps the
-         # dK/dV sweep at d = 128 within its registers (the default spills 3-18)
-         "attn_bwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]}
+EXTRA = {"attn_bf16.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]}
 
 
 # what decides an attention launch and its time: the kernels, and the choice

@@ -222,9 +222,14 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
     // this order: the rows' scalars (KV), the 2 KSTEPS operands of X and Y, the
     // transposed operands of the sums.  They complete in issue order, so each
     // product waits for all but the reads issued after its own.
-    constexpr int OPS = 2 * KSTEPS, PF = 4;            // operands of X and Y, and how far ahead
-    constexpr int SUMS = (KV ? 4 : 2) * DBLK, GF = 4;  // products of the sums (full blocks), and how far ahead
-    constexpr int GP = KV && D > 96 ? 3 : GF;          // of which before P and dS (dK/dV at d = 128: registers are short)
+    // PIPE (d <= 72, where registers allow): the products of X and Y of a block
+    // run among the exponentials of the block before it.
+    constexpr bool PIPE = D <= 96;
+    // operands of X and Y, and how far ahead they are read; products of the sums
+    // (full blocks), how far ahead theirs, and how many of these before P and
+    // dS: less in the sweeps of dK/dV whose registers would not do
+    constexpr int OPS = 2 * KSTEPS, PF = !KV || D <= 64 ? 4 : D <= 96 ? 3 : 2;
+    constexpr int SUMS = (KV ? 4 : 2) * DBLK, GF = 4, GP = KV && D > 96 ? 2 : GF;
     u32x4 ring[PF];
     // Addresses of the current stage: a register per operand where there are
     // few (one addition each per tile), otherwise derived at each read.
@@ -294,103 +299,107 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
         tail[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, b1), tail[1], 0, 0, 0);
     };
 
-    f32x16 ndv;
-    // Block kb of tile t in stage s, whose first PF operands are in flight.
-    // LASTB: the tile's last block, in whose middle tile t + 1 is awaited and
-    // tile t + NST - 1 asked for; the next block's first operands leave before
-    // its last products.
-    auto block = [&](int t, auto kb_c) {
-        constexpr int kb = decltype(kb_c)::value;
-        constexpr bool LASTB = kb == NB - 1;
-        using Off = std::integral_constant<int, 32 * kb * C::ROWB>;
-        using Next = std::integral_constant<int, LASTB ? 0 : 32 * (kb + 1) * C::ROWB>;
-        // (opaque: the addresses derived from these are not kept in registers)
-        if constexpr (C::SWIZZLED && !HOLD) asm volatile("" : "+v"(ka[0]));
-        if constexpr (kb == 0) v_stage((uint32_t)(t % NST) * C::REGION);
-        if constexpr (C::SWIZZLED && !HOLD) asm volatile("" : "+v"(va0[0][0]), "+v"(va0[0][1]));
-        f32x16 x = {}, y = KV ? f32x16{} : ndv;
-        if constexpr (KV) {
-            constexpr int O = 256 * kb;
-            const uint32_t rs_ = ra + (uint32_t)(t % NST) * C::ROWREGION;
-            u32x4 xi[4], yi[4];
-            static_for<0, 4>([&](auto g_c) {
-                constexpr int g = decltype(g_c)::value;
-                xi[g] = lds_b128<O + 32 * g>(rs_);
-                yi[g] = lds_b128<O + 128 + 32 * g>(rs_);
-            });
-            lds_wait_upto<0>();
+    f32x16 ndv;  // what Y of dQ starts from: -D of the lane's row
+    u32x4 xi[4], yi[4];  // and X and Y of dK/dV: the rows' scalars
+    auto read_rows = [&](int t, auto kb_c) {
+        constexpr int O = 256 * decltype(kb_c)::value;
+        const uint32_t base = ra + (uint32_t)(t % NST) * C::ROWREGION;
+        static_for<0, 4>([&](auto g_c) {
+            constexpr int g = decltype(g_c)::value;
+            xi[g] = lds_b128<O + 32 * g>(base);
+            yi[g] = lds_b128<O + 128 + 32 * g>(base);
+        });
+    };
+    auto start_rows = [&](f32x16& x, f32x16& y) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                asm volatile("" : "+v"(xi[g]), "+v"(yi[g]));
+        for (int g = 0; g < 4; ++g) {
+            asm volatile("" : "+v"(xi[g]), "+v"(yi[g]));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[4 * g + i] = __uint_as_float(xi[g][i]);
-                    y[4 * g + i] = __uint_as_float(yi[g][i]);
-                }
+            for (int i = 0; i < 4; ++i) {
+                x[4 * g + i] = __uint_as_float(xi[g][i]);
+                y[4 * g + i] = __uint_as_float(yi[g][i]);
             }
+        }
+    };
+    // the first reads of block kb of tile t
+    auto start_block = [&](int t, auto kb_c) {
+        constexpr int kb = decltype(kb_c)::value;
+        if constexpr (kb == 0) k_stage((uint32_t)(t % NST) * C::REGION);
+        if constexpr (KV && PIPE) read_rows(t, kb_c);
+        first_ops(std::integral_constant<int, 32 * kb * C::ROWB>{});
+    };
+    // X and Y of block kb of tile t, whose first reads are in flight;
+    // between(j) goes behind product j
+    auto products = [&](int t, auto kb_c, f32x16& x, f32x16& y, auto&& between) {
+        constexpr int kb = decltype(kb_c)::value;
+        using Off = std::integral_constant<int, 32 * kb * C::ROWB>;
+        // (opaque: the addresses derived from this are not kept in registers)
+        if constexpr (C::SWIZZLED && !HOLD) asm volatile("" : "+v"(ka[0]));
+        if constexpr (KV && !PIPE) {
+            read_rows(t, kb_c);
+            lds_wait_upto<0>();
+            start_rows(x, y);
+        }
+        if constexpr (!KV) {
+            x = f32x16{};
+            y = ndv;
         }
         static_for<0, OPS>([&](auto j_c) {
             constexpr int j = decltype(j_c)::value;
             lgkm_wait_v4<(OPS - 1 - j < PF - 1 ? OPS - 1 - j : PF - 1)>(ring[j % PF]);
+            if constexpr (KV && PIPE && j == 0) start_rows(x, y);  // read before the operand
             const bf16x8 op = __builtin_bit_cast(bf16x8, ring[j % PF]);
             if constexpr (j & 1) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, r2[j / 2], y, 0, 0, 0);
             else x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, r1[j / 2], x, 0, 0, 0);
             if constexpr (j + PF < OPS) read_op(Off{}, std::integral_constant<int, j + PF>{});
+            between(j_c);
         });
-        static_for<0, GP>([&](auto m) { read_sum(Off{}, m); });
-        if constexpr (LASTB) {
-            // tile t + 1 has landed in every wave (tile t + 2 may be in flight), and
-            // every wave is done with tile t - 1, whose stage takes tile t + NST - 1
-            wait_tiles(std::integral_constant<int, NST - 3>{});
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            load_tile(t + NST - 1, (t + NST - 1) % NST);
+    };
+    // P and dS of 16 streamed rows of block kb of tile t (values 8ks .. 8ks + 7)
+    bf16x8 pb[2], zb[2];
+    auto weights = [&](int t, auto kb_c, auto ks_c, const f32x16& x, const f32x16& y) {
+        constexpr int kb = decltype(kb_c)::value, ks = decltype(ks_c)::value;
+        float p[8], z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            p[e] = __builtin_amdgcn_exp2f(KV ? x[8 * ks + e] * a.c2 : __builtin_fmaf(x[8 * ks + e], a.c2, nl));
+        if constexpr (!KV)
+            if ((tb + t + 1) * BN > a.Nt)  // streamed keys past the end have no probability
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = 8 * ks + e;
+                    if ((tb + t) * BN + 32 * kb + krow<C::PERM>(8 * (i >> 2) + 4 * hf + (i & 3)) >= a.Nt) p[e] = 0.f;
+                }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = p[e] * y[8 * ks + e];
+        u32x4 pw, zw;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (KV) pw[w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
+            zw[w] = pack_bf16x2(z[2 * w], z[2 * w + 1]);
         }
-        bf16x8 pb[2], zb[2];
-        const bool ragged = !KV && (tb + t + 1) * BN > a.Nt;
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            float p[8], z[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = 8 * ks + e;
-                p[e] = __builtin_amdgcn_exp2f(KV ? x[i] * a.c2 : __builtin_fmaf(x[i], a.c2, nl));
-            }
-            if constexpr (!KV)
-                if (ragged)  // streamed keys past the end have no probability
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int i = 8 * ks + e;
-                        if ((tb + t) * BN + 32 * kb + krow<C::PERM>(8 * (i >> 2) + 4 * hf + (i & 3)) >= a.Nt) p[e] = 0.f;
-                    }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = p[e] * y[8 * ks + e];
-            u32x4 pw, zw;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                if constexpr (KV) pw[w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
-                zw[w] = pack_bf16x2(z[2 * w], z[2 * w + 1]);
-            }
-            if constexpr (KV) pb[ks] = __builtin_bit_cast(bf16x8, pw);
-            zb[ks] = __builtin_bit_cast(bf16x8, zw);
-        }
+        if constexpr (KV) pb[ks] = __builtin_bit_cast(bf16x8, pw);
+        zb[ks] = __builtin_bit_cast(bf16x8, zw);
+    };
+    // The sums over block kb of tile t (GP operands are in flight).  next()
+    // issues the first reads of the block after the next products' one, behind
+    // the last operand of the sums.
+    auto sums = [&](auto kb_c, auto n_next, auto&& next) {
+        constexpr int kb = decltype(kb_c)::value, NEXT = decltype(n_next)::value;  // reads that next() issues
+        using Off = std::integral_constant<int, 32 * kb * C::ROWB>;
         static_for<GP, GF>([&](auto m) { read_sum(Off{}, m); });
+        constexpr int LEFT = SUMS - GF;  // from here on no more operands are asked for, then the tails'
+        constexpr int TAILS = C::TAIL ? (KV ? 4 : 2) : 0;
         static_for<0, SUMS>([&](auto m_c) {
             constexpr int m = decltype(m_c)::value;
             constexpr bool second = KV && m < 2 * DBLK;
             constexpr int ks = m / DBLK % 2, db = m % DBLK;
-            constexpr int LEFT = SUMS - GF;  // from here on no more reads are issued, then the tails' and the next operands
             if constexpr (m == LEFT) read_tails(Off{});
-            constexpr int TAILS = C::TAIL ? (KV ? 4 : 2) : 0;
             if constexpr (m < LEFT) {
                 lds_wait_upto<2 * (GF - 1)>(gr[m % GF][0], gr[m % GF][1]);
             } else {
-                lds_wait_upto<2 * (SUMS - 1 - m) + TAILS + PF * (m > LEFT)>(gr[m % GF][0], gr[m % GF][1]);
-                if constexpr (m == LEFT) {
-                    if constexpr (LASTB) k_stage((uint32_t)((t + 1) % NST) * C::REGION);
-                    first_ops(Next{});
-                }
+                lds_wait_upto<2 * (SUMS - 1 - m) + TAILS + (m > LEFT ? NEXT : 0)>(gr[m % GF][0], gr[m % GF][1]);
+                if constexpr (m == LEFT) next();
             }
             const bf16x8 va =
                 __builtin_bit_cast(bf16x8, u32x4{gr[m % GF][0][0], gr[m % GF][0][1], gr[m % GF][1][0], gr[m % GF][1][1]});
@@ -399,11 +408,24 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
             if constexpr (m + GF < SUMS) read_sum(Off{}, std::integral_constant<int, m + GF>{});
         });
         if constexpr (C::TAIL) {
-            lds_wait_upto<PF>(gt[0][0], gt[0][1], gt[1][0], gt[1][1]);
+            lds_wait_upto<NEXT>(gt[0][0], gt[0][1], gt[1][0], gt[1][1]);
             if constexpr (KV) tail_product(gt[0], pb, tail1);
             tail_product(gt[1], zb, tail2);
         }
     };
+    // Tile t + 1 has landed in every wave (tile t + 2 may be in flight), and
+    // every wave is done with tile t - 1, whose stage takes tile t + NST - 1.
+    auto turn = [&](int t) {
+        wait_tiles(std::integral_constant<int, NST - 3>{});
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        load_tile(t + NST - 1, (t + NST - 1) % NST);
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    constexpr int FIRST_READS = PF + (KV && PIPE ? 8 : 0);  // of start_block
+
     if (ntiles > 0) {
         // the first NST-1 tiles load whether or not there are that many (past
         // the end they read zeros, into stages nobody reads)
@@ -412,9 +434,8 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
 #pragma unroll
         for (int kk = 0; kk < KSTEPS; ++kk) asm volatile("" : "+v"(r1[kk]), "+v"(r2[kk]));
         asm volatile("" : "+v"(nl), "+v"(nd));
-        // what Y of dQ starts from: -D of the lane's row, a register per value so
-        // that the first product takes it as it stands
         if constexpr (!KV) {
+            // a register per value, so that the first product takes it as it stands
 #pragma unroll
             for (int i = 0; i < 16; ++i) ndv[i] = nd;
             asm volatile("" : "+v"(ndv));
@@ -423,15 +444,56 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        k_stage(0);
-        first_ops(std::integral_constant<int, 0>{});
-        for (int t = 0; t < ntiles; ++t)
-            static_for<0, NB>([&](auto kb_c) { block(t, kb_c); });
+        f32x16 x0, y0, x1, y1;
+        auto nothing = [](auto) {};
+        using Reads = std::integral_constant<int, FIRST_READS>;
+        start_block(0, I0{});
+        if constexpr (PIPE) {
+            static_assert(!PIPE || NB == 2, "two blocks of a tile take turns");
+            products(0, I0{}, x0, y0, nothing);
+            start_block(0, I1{});
+            for (int t = 0; t < ntiles; ++t) {
+                // the exponentials of one block, eight at a time, behind the products
+                // of the next block; the sums' first operands behind the last ones
+                auto among = [&](auto kb_c, const f32x16& x, const f32x16& y) {
+                    return [&, kb_c](auto j_c) {
+                        constexpr int j = decltype(j_c)::value;
+                        if constexpr (j == 0) weights(t, kb_c, I0{}, x, y);
+                        if constexpr (j == OPS / 2) weights(t, kb_c, I1{}, x, y);
+                        if constexpr (j == OPS - 1)
+                            static_for<0, GP>([&](auto m) { read_sum(std::integral_constant<int, 32 * decltype(kb_c)::value * C::ROWB>{}, m); });
+                    };
+                };
+                v_stage((uint32_t)(t % NST) * C::REGION);
+                products(t, I1{}, x1, y1, among(I0{}, x0, y0));
+                sums(I0{}, Reads{}, [&] {
+                    turn(t);
+                    start_block(t + 1, I0{});
+                });
+                products(t + 1, I0{}, x0, y0, among(I1{}, x1, y1));
+                sums(I1{}, Reads{}, [&] { start_block(t + 1, I1{}); });
+            }
+        } else {
+            static_assert(PIPE || NB == 1, "one block per tile");
+            for (int t = 0; t < ntiles; ++t) {
+                v_stage((uint32_t)(t % NST) * C::REGION);
+                if constexpr (C::SWIZZLED && !HOLD) asm volatile("" : "+v"(va0[0][0]), "+v"(va0[0][1]));
+                products(t, I0{}, x0, y0, nothing);
+                static_for<0, GP>([&](auto m) { read_sum(I0{}, m); });
+                turn(t);
+                weights(t, I0{}, I0{}, x0, y0);
+                weights(t, I0{}, I1{}, x0, y0);
+                sums(I0{}, Reads{}, [&] { start_block(t + 1, I0{}); });
+            }
+        }
     }
     // the last block's look-ahead reads and the tiles past the end
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
     for (int j = 0; j < PF; ++j) asm volatile("" : "+v"(ring[j]));
+    if constexpr (KV && PIPE)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) asm volatile("" : "+v"(xi[g]), "+v"(yi[g]));
     wait_vmem<0>();
 
     // Results: lane c holds resident row 32 wave + c, dims 32db + 8g + 4hf + i;
