@@ -228,7 +228,7 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
     // operands of X and Y, and how far ahead they are read; products of the sums
     // (full blocks), how far ahead theirs, and how many of these before P and
     // dS: less in the sweeps of dK/dV whose registers would not do
-    constexpr int OPS = 2 * KSTEPS, PF = !KV || D <= 64 ? 4 : D <= 96 ? 3 : 2;
+    constexpr int OPS = 2 * KSTEPS, PF = !KV || D <= 64 ? 4 : 2;
     constexpr int SUMS = (KV ? 4 : 2) * DBLK, GF = 4, GP = KV && D > 96 ? 2 : GF;
     u32x4 ring[PF];
     // Addresses of the current stage: a register per operand where there are
@@ -447,8 +447,11 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
         f32x16 x0, y0, x1, y1;
         auto nothing = [](auto) {};
         using Reads = std::integral_constant<int, FIRST_READS>;
-        start_block(0, I0{});
-        if constexpr (PIPE) {
+        if (rt * kRows + wave * 32 >= a.Nr) {
+            // a wave whose rows all lie past the end only loads its share
+            for (int t = 0; t < ntiles; ++t) turn(t);
+        } else if constexpr (PIPE) {
+            start_block(0, I0{});
             static_assert(!PIPE || NB == 2, "two blocks of a tile take turns");
             products(0, I0{}, x0, y0, nothing);
             start_block(0, I1{});
@@ -475,6 +478,7 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
             }
         } else {
             static_assert(PIPE || NB == 1, "one block per tile");
+            start_block(0, I0{});
             for (int t = 0; t < ntiles; ++t) {
                 v_stage((uint32_t)(t % NST) * C::REGION);
                 if constexpr (C::SWIZZLED && !HOLD) asm volatile("" : "+v"(va0[0][0]), "+v"(va0[0][1]));
@@ -658,6 +662,58 @@ hipError_t launch_sweeps(const BwdArgs& kv, const BwdArgs& q, hipStream_t s) {
 }
 
 }  // namespace
+
+// A model of the launch in microseconds.  A workgroup takes 4 us (operands,
+// first tiles, results) plus, per block of 32 streamed rows, `unit` for each of
+// its products (4 for dK and dV, 3 for dQ) with another workgroup on its CU.
+// 512 workgroups run at once; where they are fewer, the longest decides, at 0.8
+// of its time if it has its CU to itself; more of them take their sum's share
+// and a part of the longest, which ends alone.  Cut sweeps add the join:
+// a launch, and partials written and read at 2 TB/s.
+// Measured with parts 1 and best, us: 2 x 16 heads of 72, 1024 x 1024 50 (cut
+// in 2: 54); 24 heads of 128, 512 x 4224 133, dQ in 2 107; 2 x 24 heads of 64,
+// 333 x 4429 124, dQ in 6 94; 24 heads of 64, 1 x 4429 73, dQ in 12 32; 24 heads
+// of 128, 4224 x 64 137, dK/dV in 6 47; 3 heads of 128, 4224 x 4224 132, in 3 and
+// 2 102; 8000 x 8000, one head of 64 136, in 4 and 4 67; float32, 2 heads of 64,
+// 256 x 64 25, dK/dV in 8 13.  Over 86 calls timed with all parts, the model's
+// choice takes 2.7 % more time than the best in the mean, at worst 34 %.
+BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16) {
+    BwdSplits best{1, 1, bf16 ? kRows : 64};
+    const int tile = bf16 && D <= 96 ? 64 : 32;
+    const double unit = bf16 ? (D == 64 ? 0.247 : D == 72 ? 0.296 : 0.465) : (D == 64 ? 1.15 : D == 72 ? 1.33 : 2.2);
+    constexpr int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16};
+    constexpr int64_t kSlots = 512;
+    const int64_t wgs[2] = {bh * ((Nq + best.rows - 1) / best.rows), bh * ((Nk + best.rows - 1) / best.rows)};
+    const int64_t tiles[2] = {(Nk + tile - 1) / tile, (Nq + tile - 1) / tile};
+    double each[2][8], join[2][8];
+    for (int w = 0; w < 2; ++w)
+        for (int i = 0; i < 8; ++i) {
+            const int s = kParts[i];
+            each[w][i] = s > 1 && (s > tiles[w] || s * wgs[w] > 2 * kSlots)
+                             ? -1.
+                             : 4. + (double)((tiles[w] + s - 1) / s * (tile / 32) * (w ? 4 : 3)) * unit;
+            join[w][i] = s > 1 ? 2. * (w ? 8. : 4.) * (double)(bh * (w ? Nk : Nq) * D) * s / 2e6 : 0.;
+        }
+    double least = INFINITY;
+    for (int i = 0; i < 8; ++i)
+        for (int j = 0; j < 8; ++j) {
+            const double q = each[0][i], k = each[1][j];
+            if (q < 0. || k < 0.) continue;
+            const int64_t nq = wgs[0] * kParts[i], nk = wgs[1] * kParts[j], n = nq + nk;
+            const double sum = ((double)nq * q + (double)nk * k) / kSlots;
+            const double longest = wgs[0] == 0 ? k : wgs[1] == 0 ? q : fmax(q, k);
+            double t = n <= kSlots / 2 ? 0.8 * longest
+                       : n <= kSlots   ? fmax(sum, longest * (0.8 + 0.2 * (double)(n - kSlots / 2) / (kSlots / 2)))
+                                       : sum + 0.4 * longest;
+            if (i + j > 0) t += 4. + join[0][i] + join[1][j];
+            if (t < least) {
+                least = t;
+                best.q = kParts[i];
+                best.kv = kParts[j];
+            }
+        }
+    return best;
+}
 
 hipError_t launch_bwd_join(const AttnBwdParams& p, hipStream_t s) {
     JoinArgs a{};

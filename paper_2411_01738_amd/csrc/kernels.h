@@ -142,6 +142,12 @@ hipError_t launch_norm_rope(const NormRopeParams& p, hipStream_t s);
 // (norm_rope_bwd_partials floats).
 hipError_t launch_norm_rope_bwd(const NormRopeParams& p, hipStream_t s);
 int64_t norm_rope_bwd_partials(int64_t rows, int heads0, int heads1, int D, bool bf16);
+// Into how many parts the sweeps of a gradient call are cut, and the resident
+// rows of a workgroup.
+struct BwdSplits {
+    int q, kv, rows;
+};
+BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16);
 hipError_t launch_bwd_rows(const AttnBwdParams& p, hipStream_t s);
 // both sweeps: dq, dk and dv, or the partials of the cut ones
 hipError_t launch_attn_bwd_bf16(const AttnBwdParams& p, hipStream_t s);

@@ -169,30 +169,22 @@ void weight_spans(const xdit_qk& p, Span (&w)[4]) {
     w[3] = {p.bk, p.bk ? n : 0, "bk"};
 }
 
-// How the gradients' sweeps of a call are cut: few resident tiles (128 rows of
-// one head) over a long other side leave CUs idle.  Parts are whole tiles of
-// the streamed side, at least kBwdPartTiles each.
-constexpr int64_t kBwdRows = 128, kBwdSlots = 512, kBwdPartTiles = 4;
-
-int bwd_splits(int64_t bh, int64_t resident, int64_t streamed, int64_t d) {
-    const int64_t wgs = (resident + kBwdRows - 1) / kBwdRows * bh;
-    const int64_t tiles = (streamed + (d > 96 ? 31 : 63)) / (d > 96 ? 32 : 64);
-    if (wgs <= 0) return 1;
-    int64_t s = std::min<int64_t>(kBwdSlots / wgs, tiles / kBwdPartTiles);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(s, XDIT_MAX_SPLITS));
-}
-
 int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// How the two sweeps of the gradients are cut: their workgroups share one
+// launch, and few resident rows over a long other side would leave CUs idle.
 struct BwdPlan {
     int q_splits, kv_splits;
-    int64_t rows_bytes, q_bytes, bytes;  // of the workspace: the rows' scalars, then the partials of dq, of dk and dv
+    int64_t q_wgs, kv_wgs;            // workgroups of a batch and head
+    int64_t rows_bytes, q_bytes, bytes;  // of the workspace: the rows' scalars, the partials of dq, of dk and dv
 };
 
-BwdPlan bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t d) {
+BwdPlan bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t d, int32_t dtype) {
     BwdPlan p;
-    p.q_splits = bwd_splits(B * H, Nq, Nk, d);
-    p.kv_splits = bwd_splits(B * H, Nk, Nq, d);
+    const xdit::BwdSplits s = xdit::bwd_splits(B * H, Nq, Nk, (int)d, dtype == XDIT_BF16);
+    p.q_splits = s.q, p.kv_splits = s.kv;
+    p.q_wgs = ceil_div(Nq, s.rows) * s.q, p.kv_wgs = ceil_div(Nk, s.rows) * s.kv;
     p.rows_bytes = align256(8 * B * H * Nq);
     p.q_bytes = p.q_splits > 1 ? align256(4 * p.q_splits * B * Nq * H * d) : 0;
     p.bytes = p.rows_bytes + p.q_bytes + (p.kv_splits > 1 ? align256(8 * p.kv_splits * B * Nk * H * d) : 0);
@@ -404,7 +396,7 @@ int64_t xdit_chunk_attn_bwd_workspace_bytes(int64_t batch, int64_t q_len, int64_
     clear_error();
     const char* fn = "xdit_chunk_attn_bwd_workspace_bytes";
     if (check_dtype_dim(dtype, head_dim) != XDIT_OK || check_dims(fn, batch, q_len, kv_len, heads) != XDIT_OK) return -1;
-    return bwd_plan(batch, q_len, kv_len, heads, head_dim).bytes;
+    return bwd_plan(batch, q_len, kv_len, heads, head_dim, dtype).bytes;
 }
 
 int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,
@@ -428,7 +420,7 @@ int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void*
     if (nq > 0 && lse == nullptr) return fail(XDIT_ERR_NULL, "lse is NULL");
     XDIT_TRY(check_f32(sl));
     XDIT_TRY(check_f32(se));
-    const BwdPlan plan = bwd_plan(batch, q_len, kv_len, heads, head_dim);
+    const BwdPlan plan = bwd_plan(batch, q_len, kv_len, heads, head_dim, dtype);
     if (plan.bytes > 0 && (workspace == nullptr || workspace_bytes < plan.bytes))
         return fail(XDIT_ERR_RANGE, "%s: workspace of %lld bytes needed", fn, (long long)plan.bytes);
     if (plan.bytes > 0 && ((uintptr_t)workspace & 255u)) return fail(XDIT_ERR_LAYOUT, "%s: workspace is not 256-byte aligned", fn);
@@ -440,8 +432,7 @@ int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void*
     }
     if (batch == 0 || heads == 0) return XDIT_OK;
     // a grid holds fewer than 2^32 threads: whole batches at a time
-    const int64_t sweeps = (kv_len + kBwdRows - 1) / kBwdRows * plan.kv_splits + (q_len + kBwdRows - 1) / kBwdRows * plan.q_splits;
-    const int64_t wgs = heads * std::max<int64_t>(1, std::max((q_len + 7) / 8, sweeps));
+    const int64_t wgs = heads * std::max<int64_t>(1, std::max(ceil_div(q_len, 8), plan.q_wgs + plan.kv_wgs));
     const int64_t step = std::max<int64_t>(1, (((int64_t)1 << 24) - 1) / wgs);
     for (int64_t b0 = 0; b0 < batch; b0 += step) {
         auto at = [&](const void* p, int64_t rows, int bytes) -> char* {
