@@ -531,14 +531,16 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
 }
 
 // Both sweeps in one launch: they need nothing of each other, and the shorter
-// dQ workgroups fill the CUs that the last dK/dV ones leave.  The first n_kv
-// workgroups are those of dK/dV.
+// workgroups fill the CUs that the last of the longer ones leave.  The first
+// n_first workgroups are those of the sweep whose workgroups take longer, dK/dV
+// if kv_first.
 template <int D>
-__global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs kv, BwdArgs q, int n_kv) {
+__global__ __launch_bounds__(256, 2) void attn_bwd_kernel(BwdArgs kv, BwdArgs q, int n_first, int kv_first) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[BCfg<D, true>::LDS_BYTES];
-    const int id = blockIdx.x;
-    if (id < n_kv) sweep<D, true>(kv, lds, xcd_remap(id, n_kv));
-    else sweep<D, false>(q, lds, xcd_remap(id - n_kv, gridDim.x - n_kv));
+    const int first = (int)blockIdx.x < n_first;
+    const int id = first ? blockIdx.x : blockIdx.x - n_first, n = first ? n_first : gridDim.x - n_first;
+    if (first == kv_first) sweep<D, true>(kv, lds, xcd_remap(id, n));
+    else sweep<D, false>(q, lds, xcd_remap(id, n));
 }
 
 // Per query row: -l sqrt(d) and -D = e - g . o.  A row whose l is -inf (no
@@ -655,28 +657,30 @@ int64_t workgroups(const BwdArgs& a) { return (int64_t)a.B * a.H * a.r_tiles * a
 
 template <int D>
 hipError_t launch_sweeps(const BwdArgs& kv, const BwdArgs& q, hipStream_t s) {
-    const int64_t n_kv = workgroups(kv), n = n_kv + workgroups(q);
-    if (n == 0) return hipSuccess;
-    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)n), dim3(256), 0, s, kv, q, (int)n_kv);
+    const int64_t n_kv = workgroups(kv), n_q = workgroups(q);
+    if (n_kv + n_q == 0) return hipSuccess;
+    const int kv_first = 4 * (int64_t)kv.Nt * q.splits >= 3 * (int64_t)q.Nt * kv.splits;
+    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)(n_kv + n_q)), dim3(256), 0, s, kv, q,
+                       (int)(kv_first ? n_kv : n_q), kv_first);
     return hipGetLastError();
 }
 
 }  // namespace
 
-// A model of the launch in microseconds.  A workgroup takes 4 us (operands,
+// A model of the launch in microseconds.  A workgroup takes 6 us (operands,
 // first tiles, results) plus, per block of 32 streamed rows, `unit` for each of
 // its products (4 for dK and dV, 3 for dQ) with another workgroup on its CU.
-// 512 workgroups run at once; where they are fewer, the longest decides, at 0.8
+// 512 workgroups run at once; where they are fewer, the longest decides, at 0.65
 // of its time if it has its CU to itself; more of them take their sum's share
-// and a part of the longest, which ends alone.  Cut sweeps add the join:
-// a launch, and partials written and read at 2 TB/s.
-// Measured with parts 1 and best, us: 2 x 16 heads of 72, 1024 x 1024 50 (cut
-// in 2: 54); 24 heads of 128, 512 x 4224 133, dQ in 2 107; 2 x 24 heads of 64,
-// 333 x 4429 124, dQ in 6 94; 24 heads of 64, 1 x 4429 73, dQ in 12 32; 24 heads
-// of 128, 4224 x 64 137, dK/dV in 6 47; 3 heads of 128, 4224 x 4224 132, in 3 and
-// 2 102; 8000 x 8000, one head of 64 136, in 4 and 4 67; float32, 2 heads of 64,
-// 256 x 64 25, dK/dV in 8 13.  Over 86 calls timed with all parts, the model's
-// choice takes 2.7 % more time than the best in the mean, at worst 34 %.
+// and most of one of the shorter ones, which come last, or as long as the
+// longest.  Cut sweeps add the join: a launch, and partials written and read at
+// 2 TB/s.
+// Measured in one part, and in the best, us: 2 x 16 heads of 72, 1024 x 1024 45
+// (dQ in 2: 49); 24 heads of 128, 512 x 4224 117, dQ in 2 107; 2 x 24 heads of 64, 333 x
+// 4429 88; 24 heads of 64, 1 x 4429 55, dQ in 4 27; 24 heads of 128, 4224 x 64 132, dK/dV in 6 47; 3 heads of
+// 128, 4224 x 4224 130, dQ in 2 and dK/dV in 3 103; one head of 64, 8000 x 8000 121, dQ in 4 and dK/dV in 4 66; float32, 2 heads of
+// 64, 256 x 64 25, dQ in 2 and dK/dV in 8 13.  Over 86 calls timed with all parts, the model's choice takes
+// 2.6 % more time than the best in the mean, at worst 33 %.
 BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16) {
     BwdSplits best{1, 1, bf16 ? kRows : 64};
     const int tile = bf16 && D <= 96 ? 64 : 32;
@@ -691,7 +695,7 @@ BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16) {
             const int s = kParts[i];
             each[w][i] = s > 1 && (s > tiles[w] || s * wgs[w] > 2 * kSlots)
                              ? -1.
-                             : 4. + (double)((tiles[w] + s - 1) / s * (tile / 32) * (w ? 4 : 3)) * unit;
+                             : 6. + (double)((tiles[w] + s - 1) / s * (tile / 32) * (w ? 4 : 3)) * unit;
             join[w][i] = s > 1 ? 2. * (w ? 8. : 4.) * (double)(bh * (w ? Nk : Nq) * D) * s / 2e6 : 0.;
         }
     double least = INFINITY;
@@ -701,10 +705,10 @@ BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16) {
             if (q < 0. || k < 0.) continue;
             const int64_t nq = wgs[0] * kParts[i], nk = wgs[1] * kParts[j], n = nq + nk;
             const double sum = ((double)nq * q + (double)nk * k) / kSlots;
-            const double longest = wgs[0] == 0 ? k : wgs[1] == 0 ? q : fmax(q, k);
-            double t = n <= kSlots / 2 ? 0.8 * longest
-                       : n <= kSlots   ? fmax(sum, longest * (0.8 + 0.2 * (double)(n - kSlots / 2) / (kSlots / 2)))
-                                       : sum + 0.4 * longest;
+            const double longest = wgs[0] == 0 ? k : wgs[1] == 0 ? q : fmax(q, k), shortest = fmin(q, k);
+            double t = n <= kSlots / 2 ? 0.65 * longest
+                       : n <= kSlots   ? fmax(sum, longest * (0.65 + 0.35 * (double)(n - kSlots / 2) / (kSlots / 2)))
+                                       : fmax(sum + 0.7 * shortest, longest);
             if (i + j > 0) t += 4. + join[0][i] + join[1][j];
             if (t < least) {
                 least = t;

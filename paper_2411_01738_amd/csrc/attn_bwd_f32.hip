@@ -223,13 +223,14 @@ __device__ __forceinline__ void sweep(const BwdF32Args& a, unsigned char* lds, i
     if constexpr (KV) result(a.o1, a.splits * a.part_elems, acc1, 1.f);
 }
 
-// Both sweeps in one launch, the dK/dV workgroups first.
+// Both sweeps in one launch, the longer workgroups first, as in attn_bwd.hip.
 template <int D>
-__global__ __launch_bounds__(256, 2) void attn_bwd_f32_kernel(BwdF32Args kv, BwdF32Args q, int n_kv) {
+__global__ __launch_bounds__(256, 2) void attn_bwd_f32_kernel(BwdF32Args kv, BwdF32Args q, int n_first, int kv_first) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[lds_bytes<D>()];
-    const int id = blockIdx.x;
-    if (id < n_kv) sweep<D, true>(kv, lds, xcd_remap(id, n_kv));
-    else sweep<D, false>(q, lds, xcd_remap(id - n_kv, gridDim.x - n_kv));
+    const int first = (int)blockIdx.x < n_first;
+    const int id = first ? blockIdx.x : blockIdx.x - n_first, n = first ? n_first : gridDim.x - n_first;
+    if (first == kv_first) sweep<D, true>(kv, lds, xcd_remap(id, n));
+    else sweep<D, false>(q, lds, xcd_remap(id, n));
 }
 
 BwdF32Args sweep_args(const AttnBwdParams& p, bool kv) {
@@ -256,9 +257,11 @@ BwdF32Args sweep_args(const AttnBwdParams& p, bool kv) {
 template <int D>
 hipError_t launch_sweeps(const BwdF32Args& kv, const BwdF32Args& q, hipStream_t s) {
     const int64_t n_kv = (int64_t)kv.B * kv.H * kv.r_tiles * kv.splits;
-    const int64_t n = n_kv + (int64_t)q.B * q.H * q.r_tiles * q.splits;
-    if (n == 0) return hipSuccess;
-    hipLaunchKernelGGL(attn_bwd_f32_kernel<D>, dim3((unsigned)n), dim3(256), 0, s, kv, q, (int)n_kv);
+    const int64_t n_q = (int64_t)q.B * q.H * q.r_tiles * q.splits;
+    if (n_kv + n_q == 0) return hipSuccess;
+    const int kv_first = 4 * (int64_t)kv.Nt * q.splits >= 3 * (int64_t)q.Nt * kv.splits;
+    hipLaunchKernelGGL(attn_bwd_f32_kernel<D>, dim3((unsigned)(n_kv + n_q)), dim3(256), 0, s, kv, q,
+                       (int)(kv_first ? n_kv : n_q), kv_first);
     return hipGetLastError();
 }
 
