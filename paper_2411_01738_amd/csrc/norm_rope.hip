@@ -296,29 +296,38 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
     }
 }
 
-// Sums of the partials, one output column per 16 threads' rows, in a fixed
-// order.  blockIdx.y: weight and bias of side 0, then of side 1.
+// Sums of the partials in a fixed order: a workgroup takes 16 columns, a thread
+// four of them in every 64th partial, then lanes and waves are joined.
+// blockIdx.y: weight and bias of side 0, then of side 1.
 struct NrSumArgs {
     const float* part[4];
     float* out[4];
     int slots[4];
     int D;
 };
-constexpr int kSumCols = 16, kSumRows = 16;
+constexpr int kSumCols = 16, kSumThreads = 256;
 
-__global__ __launch_bounds__(kSumCols* kSumRows) void norm_rope_sum_kernel(NrSumArgs a) {
-    __shared__ float red[kSumRows][kSumCols + 1];
-    const int tx = threadIdx.x % kSumCols, ty = threadIdx.x / kSumCols;
-    const int q = blockIdx.y, e = blockIdx.x * kSumCols + tx;
+__global__ __launch_bounds__(kSumThreads) void norm_rope_sum_kernel(NrSumArgs a) {
+    __shared__ f32x4 red[kSumThreads / 64][4];
+    const int q = blockIdx.y;
     if (a.out[q] == nullptr) return;
-    float sum = 0.f;
-    if (e < a.D)
-        for (int j = ty; j < a.slots[q]; j += kSumRows) sum += a.part[q][(int64_t)j * a.D + e];
-    red[ty][tx] = sum;
+    const int tx = threadIdx.x & 3, e = blockIdx.x * kSumCols + 4 * tx;
+    f32x4 sum = {};
+    if (e < a.D) {
+        const float* p = a.part[q] + e;
+#pragma unroll 4
+        for (int j = threadIdx.x >> 2; j < a.slots[q]; j += kSumThreads / 4) sum += *(const f32x4*)(p + (int64_t)j * a.D);
+    }
+#pragma unroll
+    for (int o = 4; o < 64; o *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], o);
+    if ((threadIdx.x & 63) < 4) red[threadIdx.x >> 6][tx] = sum;
     __syncthreads();
-    if (ty == 0 && e < a.D) {
-        for (int j = 1; j < kSumRows; ++j) sum += red[j][tx];
-        a.out[q][e] = sum;
+    if (threadIdx.x < 4 && e < a.D) {
+        for (int w = 1; w < kSumThreads / 64; ++w) sum += red[w][tx];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.out[q][e + i] = sum[i];
     }
 }
 
@@ -327,15 +336,21 @@ struct NrGrid {
     unsigned gx;
 };
 
-// Workgroups along the tokens: one token per wave, and no more waves than the
-// chip holds at once, so that a wave's weights serve several tokens.
-NrGrid nr_grid(int64_t rows, int heads0, int heads1, int G, bool bwd) {
+// Workgroups along the tokens, a token per wave at a time.  The rotation alone
+// takes as many as there are; where a norm's weights are loaded (or their
+// gradients summed), no more than run at once, with as many tokens for each.
+// Measured, us, at one round / twice that / a workgroup per 4 tokens: norms of
+// 4224 tokens, 24 + 24 heads of 128 26 / 32 / 33; 2 x 4096, 16 + 16 of 72 17 / 18 /
+// 21; 17550, 48 + 48 of 64 91 / 93 / 90; gradients of the first 44 / 53 / 56, of the last
+// 134 / 144 / 194; rotation of 17550, 48 heads of 64 49 / 51 / 44.
+NrGrid nr_grid(int64_t rows, int heads0, int heads1, int G, int norm, bool bwd) {
     NrGrid r;
     r.nb0 = (heads0 + kBatch * G - 1) / (kBatch * G);
     r.nb1 = (heads1 + kBatch * G - 1) / (kBatch * G);
     const int64_t need = (rows + kWaves - 1) / kWaves, nb = r.nb0 + r.nb1 > 0 ? r.nb0 + r.nb1 : 1;
-    const int64_t most = (bwd ? 1024 : 2048) / nb > 1 ? (bwd ? 1024 : 2048) / nb : 1;
-    r.gx = (unsigned)(need < most ? need : most);
+    const int64_t most = (bwd ? 512 : 1024) / nb > 1 ? (bwd ? 512 : 1024) / nb : 1;
+    const int64_t each = norm == 0 ? 1 : (need + most - 1) / most;
+    r.gx = (unsigned)(each > 0 ? (need + each - 1) / each : 0);
     return r;
 }
 
@@ -374,7 +389,7 @@ hipError_t launch_any(const NormRopeParams& p, bool bwd, hipStream_t s) {
     const int V = run_of(p.D, p.bf16, p.rot, p.half);
     const int64_t es = p.bf16 ? 2 : 4;
     const int64_t rows = (int64_t)p.B * p.N;
-    const NrGrid g = nr_grid(rows, p.side[0].heads, p.side[1].heads, 64 / (p.D / (2 * V)), bwd);
+    const NrGrid g = nr_grid(rows, p.side[0].heads, p.side[1].heads, 64 / (p.D / (2 * V)), p.norm, bwd);
     const dim3 grid(g.gx, (unsigned)(g.nb0 + g.nb1));
     NrArgs a{};
     for (int i = 0; i < 2; ++i) {
@@ -425,7 +440,7 @@ hipError_t launch_any(const NormRopeParams& p, bool bwd, hipStream_t s) {
         }
     }
     if (!any) return hipSuccess;
-    hipLaunchKernelGGL(norm_rope_sum_kernel, dim3((p.D + kSumCols - 1) / kSumCols, 4), dim3(kSumCols * kSumRows), 0, s, r);
+    hipLaunchKernelGGL(norm_rope_sum_kernel, dim3((p.D + kSumCols - 1) / kSumCols, 4), dim3(kSumThreads), 0, s, r);
     return hipGetLastError();
 }
 
@@ -468,7 +483,7 @@ int64_t norm_rope_bwd_partials(int64_t rows, int heads0, int heads1, int D, bool
     int64_t most = 0;
     for (int V : {4, 8}) {
         if (V == 8 && run_of(D, bf16, 0, 0) != 8) continue;
-        const NrGrid g = nr_grid(rows, heads0, heads1, 64 / (D / (2 * V)), true);
+        const NrGrid g = nr_grid(rows, heads0, heads1, 64 / (D / (2 * V)), 1, true);
         const int64_t n = (int64_t)2 * (g.nb0 + g.nb1) * g.gx * D;
         if (n > most) most = n;
     }
