@@ -52,7 +52,7 @@ extern "C" {
 enum { XDIT_BF16 = 0, XDIT_F32 = 1, XDIT_I64 = 2 }; /* XDIT_I64: positions only */
 
 /* Norms of xdit_qk_norm_rope. */
-enum { XDIT_NORM_RMS = 1, XDIT_NORM_LAYER = 2 };
+enum { XDIT_NORM_NONE = 0, XDIT_NORM_RMS = 1, XDIT_NORM_LAYER = 2 };
 
 /* Which elements of a head rotate together: neighbours (2i, 2i + 1), or
  * (i, i + rot_dim / 2). */
@@ -412,6 +412,7 @@ int xdit_rope(const void* x, const float* cos, const float* sin, void* y, const 
  * attention: each head is normalised over its head_dim elements and rotated.
  *   RMS    n = x / sqrt(mean(x^2) + eps)
  *   LAYER  n = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps)
+ *   NONE   out = rotation(x), no weights; rot_dim > 0
  *   out = rotation(n * w + b)
  * Queries and keys have weights and biases of their own.  Statistics and
  * products are float32, rounded once.
@@ -462,6 +463,25 @@ int64_t xdit_qk_norm_rope_bwd_workspace_bytes(int64_t batch, int64_t tokens, int
 int xdit_qk_norm_rope_bwd(const xdit_qk* p, const void* q, const void* k, const void* dq_out,
                           const void* dk_out, void* dq, void* dk, float* dwq, float* dwk, float* dbq,
                           float* dbk, void* workspace, int64_t workspace_bytes);
+
+/*
+ * xdit_stage_step with the queries and keys normalised and rotated between
+ * their projection and the attention:
+ *   q = x wq,  k = x wk,  v = x wv
+ *   q, k = xdit_qk_norm_rope(qk, q, k), in place
+ *   the patch step with fresh K/V = (k, v), output o
+ *   y = o wo
+ * qk describes the patch's rows: batch, tokens = patch_len, q_heads = k_heads
+ * = heads, head_dim and dtype as in the call, dense tensors (strides NULL); its
+ * table holds the patch's rows (row patch_off on of the sequence's).  q and k
+ * hold the normalised and rotated rows afterwards, as the buffer does.  Other
+ * arguments and requirements as for xdit_stage_step; no output may overlap the
+ * weights or the table.  Six launches.
+ */
+int xdit_stage_step_qk(const xdit_qk* qk, const void* x, const void* wq, const void* wk, const void* wv,
+                       const void* wo, void* kv_buf, int64_t patch_off, int64_t patch_len, void* q,
+                       void* k, void* v, void* o, void* y, int64_t batch, int64_t seq_len,
+                       int64_t heads, int64_t head_dim, int64_t hidden, int32_t dtype);
 
 /* Stream for the calling thread's later launches (a hipStream_t; NULL = the
  * default stream).  Always returns XDIT_OK. */

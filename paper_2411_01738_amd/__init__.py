@@ -330,11 +330,16 @@ def xdit_kv_update(kv_buf, patch_off: int, patch_len: int, fresh_k, fresh_v) -> 
                                _ptr(fresh_v), B, N, H, d, _dtype_code(kv_buf)))
 
 
-def xdit_stage_step(x, wq, wk, wv, wo, kv_buf, patch_off: int, q, k, v, o, y) -> None:
+def xdit_stage_step(x, wq, wk, wv, wo, kv_buf, patch_off: int, q, k, v, o, y, *, norm: str = "none", eps: float = 1e-6,
+                    norm_wq=None, norm_wk=None, norm_bq=None, norm_bk=None, cos=None, sin=None,
+                    layout: str = "interleaved") -> None:
     """One PipeFusion stage micro-step at one attention layer: q/k/v = x
     W{q,k,v} (x [B,L,C], W [C,H*d]), the patch step over kv_buf [2,B,N,H,d]
     at rows [patch_off, patch_off+L) with fresh K/V (k, v) and output o, then
-    y = o wo (wo [H*d,C]).  q, k, v, o [B,L,H,d] and y [B,L,C] are written."""
+    y = o wo (wo [H*d,C]).  q, k, v, o [B,L,H,d] and y [B,L,C] are written.
+    With a norm or a rotary table, q and k are normalised and rotated as by
+    xdit_qk_norm_rope between the projections and the patch step: cos, sin
+    hold the patch's rows, [L, r] or [B, L, r]."""
     _buffer(kv_buf)
     _, B, N, H, d = kv_buf.shape
     _dense(x, "x", 3)
@@ -352,6 +357,14 @@ def xdit_stage_step(x, wq, wk, wv, wo, kv_buf, patch_off: int, q, k, v, o, y) ->
             raise XditError(-3, f"{nm} must be {(B, L, H, d)} of x's dtype")
     if kv_buf.dtype != x.dtype:
         raise XditError(-3, "kv_buf must have x's dtype")
+    if norm != "none" or any(t is not None for t in (norm_wq, norm_wk, norm_bq, norm_bk, cos, sin)):
+        p = _qk(q, k, [], norm, eps, norm_wq, norm_wk, norm_bq, norm_bk, cos, sin, layout)
+        p.strides = None  # dense, as checked above
+        _use_current_stream()
+        check(lib().xdit_stage_step_qk(ctypes.byref(p), _ptr(x), _ptr(wq), _ptr(wk), _ptr(wv), _ptr(wo), _ptr(kv_buf),
+                                       int(patch_off), L, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(y), B, N, H, d, C,
+                                       _dtype_code(x)))
+        return
     _use_current_stream()
     check(lib().xdit_stage_step(_ptr(x), _ptr(wq), _ptr(wk), _ptr(wv), _ptr(wo), _ptr(kv_buf),
                                 int(patch_off), L, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(y), B,
@@ -429,6 +442,9 @@ def xdit_rope_table(pos, dims, cos, sin, theta: float = 10000.0, scaling: str = 
     frequencies / factor), "ntk" (theta grown so that the slowest pair is
     divided by factor) or "ramp" (by a pair's turns within orig_len: kept from
     `fast` turns on, / factor up to `slow`); magnitude multiplies the table."""
+    nat = _native if _native is not None else _load_native()
+    if nat and _done(nat.rope_table(pos, dims, cos, sin, theta, scaling, factor, orig_len, fast, slow, magnitude)):
+        return
     torch = _torch()
     dims = [int(x) for x in dims]
     if not 1 <= len(dims) <= XDIT_MAX_AXES:
@@ -504,7 +520,7 @@ def xdit_qk_norm_rope(q, k, q_out, k_out, norm: str = "rms", eps: float = 1e-6, 
                       cos=None, sin=None, layout: str = "interleaved") -> None:
     """Queries q [B, N, H, d] and keys k [B, N, Hk, d] (or None) normalised per
     head ("rms" or "layer", weights [d] and, for "layer", biases [d] of their own,
-    bfloat16 or float32) and rotated as by xdit_rope (no table: not rotated).
+    bfloat16 or float32; "none": not normalised) and rotated as by xdit_rope (no table: not rotated).
     Tensors may be strided (each head contiguous): views of one fused
     projection's output; q_out may be q and k_out k."""
     nat = _native if _native is not None else _load_native()

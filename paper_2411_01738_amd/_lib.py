@@ -20,7 +20,7 @@ STATUS = {
     -7: "XDIT_ERR_UNSUPPORTED", -8: "XDIT_ERR_HIP",
 }
 XDIT_BF16, XDIT_F32, XDIT_I64 = 0, 1, 2
-NORMS = {"rms": 1, "layer": 2}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
 LAYOUTS = {"interleaved": 0, "half": 1}
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
 XDIT_MAX_AXES = 4
@@ -78,6 +78,8 @@ SIGNATURES = {
     "xdit_qk_norm_rope_bwd_workspace_bytes": (_i64, [_i64, _i64, _i64, _i64, _i64, _i32]),
     "xdit_qk_norm_rope_bwd": (ctypes.c_int, [ctypes.POINTER(Qk), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                              _i64]),
+    "xdit_stage_step_qk": (ctypes.c_int, [ctypes.POINTER(Qk), _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp,
+                                          _vp, _i64, _i64, _i64, _i64, _i64, _i32]),
     "xdit_set_stream": (ctypes.c_int, [_vp]),
     "xdit_get_stream": (_vp, []),
     "xdit_last_error": (ctypes.c_char_p, []),

@@ -63,6 +63,17 @@ bool integer(PyObject* o, int64_t* x) {
     return true;
 }
 
+// a float or a whole number that a double holds
+bool number(PyObject* o, double* x) {
+    if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return false;
+    *x = PyFloat_AsDouble(o);
+    if (*x == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    return true;
+}
+
 // up to XDIT_MAX_RANGES (offset, length) pairs; *F their total length
 bool ranges(PyObject* o, int64_t* off, int64_t* len, int32_t* n, int64_t* F) {
     if (!PyList_CheckExact(o) && !PyTuple_CheckExact(o)) return false;
@@ -275,7 +286,7 @@ bool choice(PyObject* o, const char* const (&names)[N], int32_t first, int32_t* 
         }
     return false;
 }
-const char* const kNorms[] = {"rms", "layer"};
+const char* const kNorms[] = {"none", "rms", "layer"};
 const char* const kLayouts[] = {"interleaved", "half"};
 
 bool device_of(PyObject* o, c10::DeviceIndex dev) { return THPVariable_Unpack(o).device().index() == dev; }
@@ -316,6 +327,41 @@ bool current_device(c10::DeviceIndex* dev) {
     return true;
 }
 
+const char* const kScalings[] = {"none", "linear", "ntk", "ramp"};
+
+// pos, dims, cos, sin, theta, scaling, factor, orig_len, fast, slow, magnitude
+PyObject* rope_table(PyObject* const* a) {
+    T pos, c, s;
+    c10::DeviceIndex dev;
+    xdit_rope_scaling sc{};
+    double f[6];
+    if (!get(a[0], 2, &pos) || !get(a[2], 2, &c) || !get(a[3], 2, &s) || !PyList_CheckExact(a[1]) || !current_device(&dev) ||
+        !device_of(a[0], dev) || !device_of(a[2], dev) || !device_of(a[3], dev) || !choice(a[5], kScalings, 0, &sc.kind))
+        Py_RETURN_NONE;
+    const int at[6] = {4, 6, 7, 8, 9, 10};
+    for (int i = 0; i < 6; ++i)
+        if (!number(a[at[i]], &f[i])) Py_RETURN_NONE;
+    sc.factor = f[1], sc.orig_len = f[2], sc.fast = f[3], sc.slow = f[4], sc.magnitude = f[5];
+    const Py_ssize_t axes = PyList_GET_SIZE(a[1]);
+    int32_t dims[XDIT_MAX_AXES];
+    int64_t all = 0;
+    if (axes < 1 || axes > XDIT_MAX_AXES) Py_RETURN_NONE;
+    for (Py_ssize_t i = 0; i < axes; ++i) {
+        int64_t d;
+        if (!integer(PyList_GET_ITEM(a[1], i), &d) || d < 0 || d > 256) Py_RETURN_NONE;
+        dims[i] = (int32_t)d;
+        all += d;
+    }
+    const int64_t n = pos.s[0];
+    if (pos.s[1] != axes || (pos.dt != at::kLong && pos.dt != at::kFloat)) Py_RETURN_NONE;
+    for (const T* t : {&c, &s})
+        if (t->dt != at::kFloat || t->s[0] != n || t->s[1] != all / 2) Py_RETURN_NONE;
+    return run([&] {
+        return xdit_rope_table(pos.p, pos.dt == at::kLong ? XDIT_I64 : XDIT_F32, n, (int32_t)axes, dims, f[0], &sc, (float*)c.p,
+                               (float*)s.p);
+    });
+}
+
 // x, cos, sin, y, layout, transpose
 PyObject* rope(PyObject* const* a) {
     V x, y;
@@ -341,11 +387,10 @@ bool qk_params(const V& q, const V& k, PyObject* norm, PyObject* eps, PyObject* 
                PyObject* layout, xdit_qk* p) {
     T c, s, wt[4];
     c10::DeviceIndex dev;
-    if (!code(q.dt, &p->dtype) || !choice(norm, kNorms, XDIT_NORM_RMS, &p->norm) || !choice(layout, kLayouts, 0, &p->layout) ||
-        !PyFloat_CheckExact(eps) || !table(co, so, q, &c, &s, &p->rot_dim, &p->table_per_batch) || !current_device(&dev) ||
+    if (!code(q.dt, &p->dtype) || !choice(norm, kNorms, XDIT_NORM_NONE, &p->norm) || !choice(layout, kLayouts, 0, &p->layout) ||
+        !number(eps, &p->eps) || !table(co, so, q, &c, &s, &p->rot_dim, &p->table_per_batch) || !current_device(&dev) ||
         dev != q.dev)
         return false;
-    p->eps = PyFloat_AS_DOUBLE(eps);
     p->weight_dtype = -1;
     for (int i = 0; i < 4; ++i) {
         if (w[i] == nullptr || w[i] == Py_None) continue;
@@ -445,7 +490,7 @@ PyObject* init(PyObject* const* a) {
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))&entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(init, 2),         ENTRY(chunk, 6),       ENTRY(chunk_split, 8),
                          ENTRY(patch, 7),        ENTRY(patch_ranges, 7), ENTRY(patch_split, 9),
-                         ENTRY(merge, 5),        ENTRY(update, 5),      ENTRY(rope, 6),
+                         ENTRY(merge, 5),        ENTRY(update, 5),      ENTRY(rope_table, 11), ENTRY(rope, 6),
                          ENTRY(qk_norm_rope, 13), ENTRY(qk_norm_rope_bwd, 18), ENTRY(chunk_bwd, 13),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

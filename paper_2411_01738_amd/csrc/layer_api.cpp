@@ -118,23 +118,26 @@ int check_heads(const char* fn, int64_t B, int64_t N, int64_t H) {
     return XDIT_OK;
 }
 
-int check_qk(const char* fn, const xdit_qk* p, Span* sc, Span* ss) {
+int check_qk(const char* fn, const xdit_qk* p) {
     if (p == nullptr) return fail(XDIT_ERR_NULL, "%s: the parameters are NULL", fn);
     XDIT_TRY(check_dtype_dim(p->dtype, p->head_dim));
     if (p->weight_dtype != XDIT_BF16 && p->weight_dtype != XDIT_F32)
         return fail(XDIT_ERR_DTYPE, "%s: unknown weight_dtype %d", fn, p->weight_dtype);
     XDIT_TRY(check_heads(fn, p->batch, p->tokens, p->q_heads));
     XDIT_TRY(check_heads(fn, p->batch, p->tokens, p->k_heads));
-    if (p->norm != XDIT_NORM_RMS && p->norm != XDIT_NORM_LAYER)
+    if (p->norm < XDIT_NORM_NONE || p->norm > XDIT_NORM_LAYER)
         return fail(XDIT_ERR_RANGE, "%s: unknown norm %d", fn, p->norm);
+    if (p->norm == XDIT_NORM_NONE && (p->wq || p->wk || p->bq || p->bk || p->rot_dim == 0))
+        return fail(XDIT_ERR_RANGE, "%s: without a norm there are no weights, and a rotation", fn);
     if (p->norm == XDIT_NORM_RMS && (p->bq || p->bk)) return fail(XDIT_ERR_RANGE, "%s: the RMS norm has no bias", fn);
     if (!(p->eps >= 0.0) || !std::isfinite((float)p->eps))
         return fail(XDIT_ERR_RANGE, "%s: eps = %g is no float32 number from 0 on", fn, p->eps);
     for (const void* w : {p->wq, p->wk, p->bq, p->bk})
         if (w && ((uintptr_t)w & (p->weight_dtype == XDIT_BF16 ? 1u : 3u)))
             return fail(XDIT_ERR_LAYOUT, "%s: a weight is not aligned to its type", fn);
+    Span sc, ss;
     return check_rotation(fn, p->cos, p->sin, p->rot_dim, p->head_dim, p->layout,
-                          p->tokens * (p->table_per_batch ? p->batch : 1), sc, ss);
+                          p->tokens * (p->table_per_batch ? p->batch : 1), &sc, &ss);
 }
 
 xdit::NormRopeParams params_of(const xdit_qk& p) {
@@ -158,15 +161,6 @@ xdit::NormRopeParams params_of(const xdit_qk& p) {
     r.half = p.layout == XDIT_PAIRS_HALF;
     r.eps = (float)p.eps;
     return r;
-}
-
-// Spans of weights and biases, which no output may overlap.
-void weight_spans(const xdit_qk& p, Span (&w)[4]) {
-    const int64_t n = p.head_dim * (p.weight_dtype == XDIT_BF16 ? 2 : 4);
-    w[0] = {p.wq, p.wq ? n : 0, "wq"};
-    w[1] = {p.wk, p.wk ? n : 0, "wk"};
-    w[2] = {p.bq, p.bq ? n : 0, "bq"};
-    w[3] = {p.bk, p.bk ? n : 0, "bk"};
 }
 
 int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
@@ -195,25 +189,55 @@ BwdPlan bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t d, int32_
 
 namespace xdit_api {
 
-int qk_norm_rope(const char* fn, const xdit_qk* p, const void* q, const void* k, void* q_out, void* k_out) {
-    Span sc, ss, sw[4];
-    XDIT_TRY(check_qk(fn, p, &sc, &ss));
+void qk_spans(const xdit_qk& p, Span (&s)[6]) {
+    const int64_t n = p.head_dim * (p.weight_dtype == XDIT_BF16 ? 2 : 4);
+    const int64_t t = p.tokens * (p.table_per_batch ? p.batch : 1) * (p.rot_dim / 2) * 4;
+    s[0] = {p.wq, p.wq ? n : 0, "wq"};
+    s[1] = {p.wk, p.wk ? n : 0, "wk"};
+    s[2] = {p.bq, p.bq ? n : 0, "bq"};
+    s[3] = {p.bk, p.bk ? n : 0, "bk"};
+    s[4] = {p.cos, t, "cos"};
+    s[5] = {p.sin, t, "sin"};
+}
+
+}  // namespace xdit_api
+
+namespace {
+
+// Checks of a forward call; its views in argument order.
+int check_forward(const char* fn, const xdit_qk* p, const void* q, const void* k, void* q_out, void* k_out, View (&v)[4]) {
+    XDIT_TRY(check_qk(fn, p));
     const int es = esize_of(p->dtype);
     const int64_t *st = p->strides, heads[4] = {p->q_heads, p->k_heads, p->q_heads, p->k_heads};
     const void* ptr[4] = {q, k, q_out, k_out};
     const char* names[4] = {"q", "k", "q_out", "k_out"};
-    View v[4];
     for (int i = 0; i < 4; ++i) {
         v[i] = view(ptr[i], p->batch, p->tokens, heads[i], p->head_dim, es, st ? st + 3 * i : nullptr, names[i]);
         XDIT_TRY(check_view(v[i]));
     }
-    weight_spans(*p, sw);
+    Span sp[6];
+    qk_spans(*p, sp);
     for (int o = 2; o < 4; ++o) {
         XDIT_TRY(check_written(v[o]));
         for (int i = 0; i < o; ++i)
             if (i != o - 2 || !same_view(v[o], v[i])) XDIT_TRY(check_apart(v[o], v[i]));
-        for (const Span& s : {sc, ss, sw[0], sw[1], sw[2], sw[3]}) XDIT_TRY(check_no_overlap(v[o].span(), s));
+        for (const Span& s : sp) XDIT_TRY(check_no_overlap(v[o].span(), s));
     }
+    return XDIT_OK;
+}
+
+}  // namespace
+
+namespace xdit_api {
+
+int check_qk_call(const char* fn, const xdit_qk* p, const void* q, const void* k, void* q_out, void* k_out) {
+    View v[4];
+    return check_forward(fn, p, q, k, q_out, k_out, v);
+}
+
+int qk_norm_rope(const char* fn, const xdit_qk* p, const void* q, const void* k, void* q_out, void* k_out) {
+    View v[4];
+    XDIT_TRY(check_forward(fn, p, q, k, q_out, k_out, v));
     if (p->batch == 0 || p->tokens == 0) return XDIT_OK;
     xdit::NormRopeParams r = params_of(*p);
     for (int i = 0; i < 2; ++i) {
@@ -335,8 +359,7 @@ int xdit_qk_norm_rope_bwd(const xdit_qk* p, const void* q, const void* k, const 
                           float* dbk, void* workspace, int64_t workspace_bytes) {
     clear_error();
     const char* fn = "xdit_qk_norm_rope_bwd";
-    Span sc, ss, sw[4];
-    XDIT_TRY(check_qk(fn, p, &sc, &ss));
+    XDIT_TRY(check_qk(fn, p));
     const int es = esize_of(p->dtype);
     const int64_t* st = p->strides;
     const void* ptr[6] = {q, k, dq_out, dk_out, dq, dk};
@@ -347,10 +370,12 @@ int xdit_qk_norm_rope_bwd(const xdit_qk* p, const void* q, const void* k, const 
                     st ? st + 3 * i : nullptr, names[i]);
         XDIT_TRY(check_view(v[i]));
     }
+    if ((dwq || dwk) && p->norm == XDIT_NORM_NONE) return fail(XDIT_ERR_RANGE, "%s: without a norm there are no weights", fn);
     if ((dbq || dbk) && p->norm != XDIT_NORM_LAYER)
-        return fail(XDIT_ERR_RANGE, "%s: the RMS norm has no bias", fn);
+        return fail(XDIT_ERR_RANGE, "%s: only the layer norm has a bias", fn);
     if (p->k_heads == 0 && (dwk || dbk)) return fail(XDIT_ERR_SHAPE, "%s: no keys, but a gradient of their weights", fn);
-    weight_spans(*p, sw);
+    Span ins[6];
+    qk_spans(*p, ins);
     const bool sums = dwq || dwk || dbq || dbk;
     const int64_t need = sums ? 4 * xdit::norm_rope_bwd_partials(p->batch * p->tokens, (int)p->q_heads, (int)p->k_heads,
                                                                  (int)p->head_dim, p->dtype == XDIT_BF16)
@@ -366,7 +391,6 @@ int xdit_qk_norm_rope_bwd(const xdit_qk* p, const void* q, const void* k, const 
                         {workspace, need, "workspace"}};
     for (int i = 0; i < 4; ++i) XDIT_TRY(check_f32(so[i]));
     XDIT_TRY(check_ptr(so[4]));
-    const Span ins[] = {sc, ss, sw[0], sw[1], sw[2], sw[3]};
     for (int o = 4; o < 6; ++o) {
         XDIT_TRY(check_written(v[o]));
         for (int i = 0; i < o; ++i)
@@ -388,7 +412,13 @@ int xdit_qk_norm_rope_bwd(const xdit_qk* p, const void* q, const void* k, const 
         r.side[i].db = grads[i][1];
     }
     r.part = (float*)workspace;
-    return hip_status(xdit::launch_norm_rope_bwd(r, g_stream), fn);
+    if (p->norm != XDIT_NORM_NONE) return hip_status(xdit::launch_norm_rope_bwd(r, g_stream), fn);
+    // the rotation alone: the gradients turned back
+    if (p->batch == 0 || p->tokens == 0) return XDIT_OK;
+    r.side[0].x = r.side[0].g;
+    r.side[1].x = r.side[1].g;
+    r.transpose = 1;
+    return hip_status(xdit::launch_norm_rope(r, g_stream), fn);
 }
 
 int64_t xdit_chunk_attn_bwd_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads,

@@ -14,8 +14,8 @@
 #include <mutex>
 #include <tuple>
 
-#include "api_common.h"
 #include "kernels.h"
+#include "layer_api.h"
 
 using namespace xdit_api;
 
@@ -780,13 +780,13 @@ int gemm_bf16(const char* fn, const void* A, const void* B, void* C, int64_t M, 
 
 }  // namespace
 
-extern "C" int xdit_stage_step(const void* x, const void* wq, const void* wk, const void* wv,
-                               const void* wo, void* kv_buf, int64_t patch_off, int64_t patch_len,
-                               void* q, void* k, void* v, void* o, void* y, int64_t batch,
-                               int64_t seq_len, int64_t heads, int64_t head_dim, int64_t hidden,
-                               int32_t dtype) {
-    clear_error();
-    const char* fn = "xdit_stage_step";
+namespace {
+
+// The stage micro-step; qk: the norms and rotation between the projections and
+// the attention, or nullptr.
+int stage_impl(const char* fn, const xdit_qk* qk, const void* x, const void* wq, const void* wk, const void* wv,
+               const void* wo, void* kv_buf, int64_t patch_off, int64_t patch_len, void* q, void* k, void* v, void* o,
+               void* y, int64_t batch, int64_t seq_len, int64_t heads, int64_t head_dim, int64_t hidden, int32_t dtype) {
     XDIT_TRY(check_dtype_dim(dtype, head_dim));
     if (dtype != XDIT_BF16) return fail(XDIT_ERR_UNSUPPORTED, "%s: bf16 only", fn);
     if (hidden <= 0 || hidden > 65536) return fail(XDIT_ERR_SHAPE, "%s: hidden = %lld outside [1, 65536]", fn,
@@ -807,6 +807,18 @@ extern "C" int xdit_stage_step(const void* x, const void* wq, const void* wk, co
         for (const Span* s : ins) XDIT_TRY(check_no_overlap(*outs[i], *s));
         for (int j = 0; j < i; ++j) XDIT_TRY(check_no_overlap(*outs[i], *outs[j]));
     }
+    if (qk) {
+        if (qk->batch != batch || qk->tokens != patch_len || qk->q_heads != heads || qk->k_heads != heads ||
+            qk->head_dim != head_dim || qk->dtype != dtype || qk->strides != nullptr)
+            return fail(XDIT_ERR_SHAPE, "%s: qk does not describe the call's dense queries and keys", fn);
+        XDIT_TRY(check_qk_call(fn, qk, q, k, q, k));
+        Span ss[6];
+        qk_spans(*qk, ss);
+        for (const Span& s : ss) {
+            XDIT_TRY(check_no_overlap(sb, s));
+            for (const Span* out : outs) XDIT_TRY(check_no_overlap(*out, s));
+        }
+    }
     if (M == 0 || heads == 0) return XDIT_OK;
     // The three projections as one strided-batched GEMM when the weights
     // are consecutive [3, C, H*d] and q, k, v consecutive [3, B, L, H, d];
@@ -824,7 +836,31 @@ extern "C" int xdit_stage_step(const void* x, const void* wq, const void* wk, co
     } else {
         XDIT_TRY(rc);
     }
+    if (qk) XDIT_TRY(qk_norm_rope(fn, qk, q, k, q, k));
     XDIT_TRY(patch_ranges_impl(fn, q, patch_len, kv_buf, 1, &patch_off, &patch_len, k, v, o, nullptr, batch,
                                seq_len, heads, head_dim, dtype));
     return gemm_bf16(fn, o, wo, y, M, hidden, HD);
 }
+
+}  // namespace
+
+extern "C" {
+
+int xdit_stage_step(const void* x, const void* wq, const void* wk, const void* wv, const void* wo, void* kv_buf,
+                    int64_t patch_off, int64_t patch_len, void* q, void* k, void* v, void* o, void* y, int64_t batch,
+                    int64_t seq_len, int64_t heads, int64_t head_dim, int64_t hidden, int32_t dtype) {
+    clear_error();
+    return stage_impl("xdit_stage_step", nullptr, x, wq, wk, wv, wo, kv_buf, patch_off, patch_len, q, k, v, o, y, batch,
+                      seq_len, heads, head_dim, hidden, dtype);
+}
+
+int xdit_stage_step_qk(const xdit_qk* qk, const void* x, const void* wq, const void* wk, const void* wv, const void* wo,
+                       void* kv_buf, int64_t patch_off, int64_t patch_len, void* q, void* k, void* v, void* o, void* y,
+                       int64_t batch, int64_t seq_len, int64_t heads, int64_t head_dim, int64_t hidden, int32_t dtype) {
+    clear_error();
+    if (qk == nullptr) return fail(XDIT_ERR_NULL, "xdit_stage_step_qk: qk is NULL");
+    return stage_impl("xdit_stage_step_qk", qk, x, wq, wk, wv, wo, kv_buf, patch_off, patch_len, q, k, v, o, y, batch,
+                      seq_len, heads, head_dim, hidden, dtype);
+}
+
+}  // extern "C"

@@ -75,6 +75,20 @@ def test_table(n, dims, kw, kind):
         assert (err <= 2.0 ** -24 * np.abs(want) + ang + 1e-12).all(), f"{what}: {err.max():.3e}"
 
 
+def test_far_positions_stay_on_the_circle():
+    """Angles so large that their own rounding is a turn have no meaning, but
+    their cosine and sine are those of some angle; infinities give NaN."""
+    torch = torch_mod()
+    pos = torch.tensor([[1 << 40], [1 << 52], [(1 << 62) + 12345], [-(1 << 60)], [2 ** 63 - 1]], device="cuda")
+    cos, sin = torch.empty(5, 64, device="cuda"), torch.empty(5, 64, device="cuda")
+    xd.xdit_rope_table(pos, [128], cos, sin)
+    assert ((cos.double() ** 2 + sin.double() ** 2 - 1).abs() < 1e-6).all()
+    bad = torch.tensor([[float("inf")], [float("nan")], [1e30], [3.0], [-0.5]], device="cuda")
+    xd.xdit_rope_table(bad, [128], cos, sin)
+    assert torch.isnan(cos[:2]).all() and torch.isnan(sin[:2]).all()
+    assert ((cos[2:].double() ** 2 + sin[2:].double() ** 2 - 1).abs() < 1e-6).all()
+
+
 def test_table_of_no_rows():
     torch = torch_mod()
     e = torch.empty(0, 32, device="cuda")
@@ -241,6 +255,24 @@ def test_heads_of_zeros_and_one_value():
     assert torch.isnan(y[0, 1, 0]).all() and not torch.isnan(y[0, 1, 1]).any() and not torch.isnan(y[0, 0]).any()
 
 
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+def test_rotation_of_queries_and_keys(layout):
+    """norm "none": both rotated in one call, and turned back by its gradient."""
+    torch = torch_mod()
+    r = Draws(15)
+    q, k = r(2, 40, 6, 72), r(2, 40, 2, 72)
+    cos, sin = r.angles(40, 20)
+    want, got = [torch.empty_like(q), torch.empty_like(k)], [torch.empty_like(q), torch.empty_like(k)]
+    for back in (False, True):
+        for x, y in zip((q, k), want):
+            xd.xdit_rope(x, cos, sin, y, layout=layout, transpose=back)
+        if back:
+            xd.xdit_qk_norm_rope_bwd(q, k, q, k, *got, norm="none", cos=cos, sin=sin, layout=layout)
+        else:
+            xd.xdit_qk_norm_rope(q, k, *got, norm="none", cos=cos, sin=sin, layout=layout)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_no_rows():
     """No rows leave zero gradients of the weights, and write nothing else."""
     torch = torch_mod()
@@ -336,6 +368,8 @@ def test_both_call_paths_agree(monkeypatch):
         out += [torch.zeros(B, N, Hk, d, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
         out += [torch.zeros(d, device="cuda") for _ in range(4)]
         ws = torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(q, k), device="cuda", dtype=torch.uint8)
+        out += [torch.zeros(N, 36, device="cuda") for _ in range(2)]
+        xd.xdit_rope_table(torch.arange(3 * N, device="cuda").view(N, 3), [16, 16, 40], out[9], out[10], scaling="ntk", factor=2.0)
         xd.xdit_rope(q, cos, sin, out[0], layout="half", transpose=True)
         xd.xdit_qk_norm_rope(q, k, out[1], out[3], norm="layer", wq=wq, wk=wk, bq=bq, bk=bk, cos=cos, sin=sin, layout="half")
         xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, out[2], out[4], norm="layer", wq=wq, wk=wk, cos=cos, sin=sin, layout="half",
@@ -356,7 +390,7 @@ def test_both_call_paths_agree(monkeypatch):
     rec = Taken()
     monkeypatch.setattr(xd, "_native", rec)
     fast = calls()
-    assert rec.names == [("rope", 0), ("qk_norm_rope", 0), ("qk_norm_rope_bwd", 0)]
+    assert rec.names == [("rope_table", 0), ("rope", 0), ("qk_norm_rope", 0), ("qk_norm_rope_bwd", 0)]
     monkeypatch.setattr(xd, "_native", False)
     for a, b in zip(fast, calls()):
         assert torch.equal(a, b)
@@ -371,13 +405,22 @@ def test_refusals_on_the_gpu(monkeypatch):
     c, w, f32 = z(5, 16, dt=torch.float32), z(64), torch.float32
     ws = z(1 << 20, dt=torch.uint8)
     norm, bwd = xd.xdit_qk_norm_rope, xd.xdit_qk_norm_rope_bwd
+    pos, tab = torch.arange(5, device="cuda").view(5, 1), xd.xdit_rope_table
     bad = [lambda: xd.xdit_rope(q, c, c, qo, layout="other"), lambda: xd.xdit_rope(q, c[:4], c[:4], qo),
            lambda: xd.xdit_rope(q, c, c[:, :8].contiguous(), qo), lambda: xd.xdit_rope(q, c, None, qo),
            lambda: xd.xdit_rope(q, z(5, 36, dt=f32), z(5, 36, dt=f32), qo), lambda: xd.xdit_rope(q, c, c, qo.float()),
            lambda: xd.xdit_rope(q, z(5, 6, dt=f32), z(5, 6, dt=f32), qo), lambda: xd.xdit_rope(q.half(), c, c, qo.half()),
            lambda: xd.xdit_rope(q[..., :32], c, c, qo[..., :32]), lambda: xd.xdit_rope(q, c, c, z(1, 1, 2, 64).expand(1, 5, 2, 64)),
            lambda: xd.xdit_rope(z(6, 2, 64)[None, :5], c, c, z(1, 5, 2, 65)[..., 1:]),
-           lambda: norm(q, k, qo, ko, norm="none"), lambda: norm(q, k, qo, ko, bq=w), lambda: norm(q, k, qo, ko, eps=-1.0),
+           lambda: tab(pos, [30], c, c.clone()), lambda: tab(pos, [32], c, c), lambda: tab(pos.int(), [32], c, c.clone()),
+           lambda: tab(pos, [16, 16], c, c.clone()), lambda: tab(pos, [31], c, c.clone()), lambda: tab(pos[:4], [32], c, c.clone()),
+           lambda: tab(pos, [32], c, c.clone(), scaling="yes"), lambda: tab(pos, [32], c, c.clone(), theta=0.0),
+           lambda: tab(pos, [32], c, c.clone(), scaling="ramp", factor=2.0),
+           lambda: tab(pos, [32], c, c.clone(), scaling="linear", factor=0.0), lambda: tab(pos.cpu(), [32], c, c.clone()),
+           lambda: tab(pos, [32], c, c.clone(), magnitude=float("inf")), lambda: tab(pos, [], c, c.clone()),
+           lambda: norm(q, k, qo, ko, norm="other"), lambda: norm(q, k, qo, ko, norm="none"),
+           lambda: norm(q, k, qo, ko, norm="none", wq=w, cos=c, sin=c), lambda: bwd(q, k, q, k, qo, ko, norm="none"),
+           lambda: bwd(q, k, q, k, qo, ko, norm="none", cos=c, sin=c, dwq=z(64, dt=f32), workspace=ws), lambda: norm(q, k, qo, ko, bq=w), lambda: norm(q, k, qo, ko, eps=-1.0),
            lambda: norm(q, k, qo, ko, eps=float("nan")), lambda: norm(q, k, qo, None), lambda: norm(q, None, qo, ko),
            lambda: norm(q, k, qo, qo), lambda: norm(q, k, k, ko), lambda: norm(q, k, qo, ko, wq=w, wk=w.float()),
            lambda: norm(q, k, qo, ko, wq=w[:32]), lambda: norm(q, k, qo, ko, cos=c), lambda: norm(q, q.cpu(), qo, ko),

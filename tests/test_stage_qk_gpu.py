@@ -1,0 +1,89 @@
+"""The stage micro-step with norms and rotation of queries and keys: the bits
+of its parts called one after another, and the formulas in 64 bits.
+
+Bounds: a projection is good to half a bf16 step (2^-8) plus float32 sums; the
+norm divides by the deviation of values with that error, at most twice it
+relative to the largest value of the head, and rounds once more."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+import paper_2411_01738_amd as xd
+from tests import layer_ref as ref
+from tests.gpu_util import to_np, torch_mod
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("B,L,N,H,d,C,off,norm,rot,layout", [
+    (2, 96, 320, 2, 72, 160, 64, "rms", 72, "half"), (1, 130, 300, 3, 64, 192, 170, "layer", 48, "interleaved"),
+    (2, 64, 256, 2, 128, 256, 0, "rms", 0, "interleaved"), (1, 1, 128, 2, 64, 64, 127, "none", 64, "interleaved")])
+def test_stage_step_qk(B, L, N, H, d, C, off, norm, rot, layout):
+    torch = torch_mod()
+    g = torch.Generator().manual_seed(400 + L)
+    r = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).bfloat16().cuda()
+    x, wo = r(B, L, C), r(H * d, C, scale=1 / math.sqrt(H * d))
+    wq, wk, wv = (r(C, H * d, scale=1 / math.sqrt(C)) for _ in range(3))
+    kv0 = r(2, B, N, H, d)
+    kw = dict(norm=norm, eps=1e-5, layout=layout)
+    if norm != "none":
+        kw.update(wq=1 + r(d, scale=0.3), wk=1 + r(d, scale=0.3))
+    if norm == "layer":
+        kw.update(bq=r(d, scale=0.2), bk=r(d, scale=0.2))
+    if rot:
+        table = [torch.empty(N, rot // 2, device="cuda") for _ in range(2)]
+        xd.xdit_rope_table(torch.arange(N, device="cuda")[:, None], [rot], *table)
+        kw.update(cos=table[0][off:off + L], sin=table[1][off:off + L])
+    stage_kw = {("norm_" + n if n[0] in "wb" else n): v for n, v in kw.items()}
+
+    def buffers():
+        return [torch.full((B, L, H, d), float("nan"), device="cuda", dtype=torch.bfloat16) for _ in range(4)] + [
+            torch.full((B, L, C), float("nan"), device="cuda", dtype=torch.bfloat16)]
+
+    q, k, v, o, y = buffers()
+    kv = kv0.clone()
+    xd.xdit_stage_step(x, wq, wk, wv, wo, kv, off, q, k, v, o, y, **stage_kw)
+    # its parts: the projections of the plain step, the norms and rotation, the patch step
+    q1, k1, v1, o1, y1 = buffers()
+    xd.xdit_stage_step(x, wq, wk, wv, wo, kv0.clone(), off, q1, k1, v1, o1, y1)
+    raw = q1.clone(), k1.clone()
+    xd.xdit_qk_norm_rope(q1, k1, q1, k1, **kw)
+    kv1 = kv0.clone()
+    xd.xdit_patch_attn(q1, kv1, off, L, k1, v1, o1)
+    for a, b in ((q, q1), (k, k1), (v, v1), (o, o1), (kv, kv1)):
+        assert torch.equal(a, b)
+    # y = o wo as the plain step forms it
+    assert np.abs(to_np(y) - to_np(o).reshape(B, L, H * d).astype(np.float64) @ to_np(wo).astype(np.float64)).max() <= 3e-2
+    f = lambda t: None if t is None else to_np(t).astype(np.float64)
+    c, s = (None, None) if not rot else (kw["cos"].cpu().numpy(), kw["sin"].cpu().numpy())
+    for got, w, wn, bn, raw_t in ((q, wq, "wq", "bq", raw[0]), (k, wk, "wk", "bk", raw[1])):
+        X = (f(x) @ f(w)).reshape(B, L, H, d)
+        W, Bn = f(kw.get(wn)), f(kw.get(bn))
+        if norm == "none":
+            want, scale = ref.rotate(X, c, s, layout), 2 * np.abs(X).max(-1, keepdims=True)
+        else:
+            want, scale = ref.forward(X, W, Bn, c, s, norm, 1e-5, layout), ref.forward_scale(X, W, Bn, norm, 1e-5)
+        err = np.abs(f(got) - want)
+        assert (err <= 2.0 ** -8 * np.abs(want) + 3 * 2.0 ** -8 * scale).all(), err.max()
+        assert np.sqrt((err ** 2).mean()) <= 2.0 ** -7 * np.sqrt((want ** 2).mean())
+
+
+def test_refusals():
+    torch = torch_mod()
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, device="cuda", dtype=dt)
+    B, L, N, H, d, C = 1, 8, 16, 2, 64, 64
+    x, w, wo, kv, y = z(B, L, C), z(C, H * d), z(H * d, C), z(2, B, N, H, d), z(B, L, C)
+    q, k, v, o = (z(B, L, H, d) for _ in range(4))
+    t = z(L, 32, dt=torch.float32)
+    step = lambda **kw: xd.xdit_stage_step(x, w, w, w, wo, kv, 4, q, k, v, o, y, **kw)
+    for kw in (dict(norm="other"), dict(norm="rms", norm_bq=z(d)), dict(norm_wq=z(d)), dict(norm="rms", cos=t), dict(cos=t[:4], sin=t[:4]),
+               dict(norm="rms", norm_wq=z(32)), dict(norm="rms", norm_wq=q[0, 0, 0]), dict(norm="rms", eps=-1.0),
+               dict(norm="rms", norm_wk=kv[0, 0, 0, 0])):
+        with pytest.raises(xd.XditError):
+            step(**kw)
+            pytest.fail(f"{list(kw)} was taken")
+    torch.cuda.synchronize()
+    assert not any(a.any() for a in (q, k, v, o, y, kv))
