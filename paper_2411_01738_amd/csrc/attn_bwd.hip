@@ -12,7 +12,9 @@
 // queries x keys is stored.  P and dS are rounded to bf16 as operands of the
 // matrix cores (half a step, 2^-8 relative, each; the sums are float32).
 //
-// What bounds it: the matrix cores.  One sweep gives dK and dV (four products
+// What bounds it: the matrix cores (24 heads of 128, 4224 x 4224: 690 us, 1110
+// TFLOP/s over the seven products, where a large product of random values
+// reaches 1372).  One sweep gives dK and dV (four products
 // of queries x keys x d), another dQ (three), seven in place of the five that
 // are needed: a single sweep would have to add its part of the other side's
 // gradient to memory for every tile, by atomics whose order changes the result
@@ -676,11 +678,13 @@ hipError_t launch_sweeps(const BwdArgs& kv, const BwdArgs& q, hipStream_t s) {
 // longest.  Cut sweeps add the join: a launch, and partials written and read at
 // 2 TB/s.
 // Measured in one part, and in the best, us: 2 x 16 heads of 72, 1024 x 1024 45
-// (dQ in 2: 49); 24 heads of 128, 512 x 4224 117, dQ in 2 107; 2 x 24 heads of 64, 333 x
-// 4429 88; 24 heads of 64, 1 x 4429 55, dQ in 4 27; 24 heads of 128, 4224 x 64 132, dK/dV in 6 47; 3 heads of
-// 128, 4224 x 4224 130, dQ in 2 and dK/dV in 3 103; one head of 64, 8000 x 8000 121, dQ in 4 and dK/dV in 4 66; float32, 2 heads of
-// 64, 256 x 64 25, dQ in 2 and dK/dV in 8 13.  Over 86 calls timed with all parts, the model's choice takes
-// 2.6 % more time than the best in the mean, at worst 33 %.
+// (dQ in 2: 49); 24 heads of 128, 512 x 4224 117, dQ in 2 107; 2 x 24 heads of
+// 64, 333 x 4429 88; 24 heads of 64, 1 x 4429 55, dQ in 4 27; 24 heads of 128,
+// 4224 x 64 132, dK/dV in 6 47; 3 heads of 128, 4224 x 4224 130, dQ in 2 and
+// dK/dV in 3 103; one head of 64, 8000 x 8000 121, dQ in 4 and dK/dV in 4 66;
+// float32, 2 heads of 64, 256 x 64 25, dQ in 2 and dK/dV in 8 13.  Over 86 calls
+// timed with all parts, the model's choice takes 2.6 % more time than the best in
+// the mean, at worst 33 %.
 BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16) {
     BwdSplits best{1, 1, bf16 ? kRows : 64};
     const int tile = bf16 && D <= 96 ? 64 : 32;

@@ -14,7 +14,10 @@
 // All of it in float32, rounded once at the store.
 //
 // What bounds it: memory.  Each head is read and written once; the tables are
-// read once per token and batch of heads.
+// read once per token and batch of heads.  bf16, where a large copy reaches 5.1
+// TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 26 us (4.0
+// TB/s); gradients of layer norms and rotation of 17550 tokens, 48 + 48 heads of
+// 64, 130 us (5.0 TB/s); rotation of one such tensor 44 us (5.0 TB/s).
 //
 // Work: a lane holds 2 V values of a head, both elements of each of its
 // pairs, so the rotation needs no other lane: the runs [2 V p, 2 V p + 2 V) for
@@ -337,19 +340,20 @@ struct NrGrid {
 };
 
 // Workgroups along the tokens, a token per wave at a time.  The rotation alone
-// takes as many as there are; where a norm's weights are loaded (or their
-// gradients summed), no more than run at once, with as many tokens for each.
+// takes as many as there are (up to 2^31 threads: a launch holds fewer than
+// 2^32); where a norm's weights are loaded (or their gradients summed), no more
+// than run at once, with as many tokens for each.
 // Measured, us, at one round / twice that / a workgroup per 4 tokens: norms of
-// 4224 tokens, 24 + 24 heads of 128 26 / 32 / 33; 2 x 4096, 16 + 16 of 72 17 / 18 /
-// 21; 17550, 48 + 48 of 64 91 / 93 / 90; gradients of the first 44 / 53 / 56, of the last
-// 134 / 144 / 194; rotation of 17550, 48 heads of 64 49 / 51 / 44.
+// 4224 tokens, 24 + 24 heads of 128 26 / 32 / 33; 2 x 4096, 16 + 16 of 72 17 / 18
+// / 21; 17550, 48 + 48 of 64 91 / 93 / 90; gradients of the first 44 / 53 / 56, of
+// the last 134 / 144 / 194; rotation of 17550, 48 heads of 64 49 / 51 / 44.
 NrGrid nr_grid(int64_t rows, int heads0, int heads1, int G, int norm, bool bwd) {
     NrGrid r;
     r.nb0 = (heads0 + kBatch * G - 1) / (kBatch * G);
     r.nb1 = (heads1 + kBatch * G - 1) / (kBatch * G);
     const int64_t need = (rows + kWaves - 1) / kWaves, nb = r.nb0 + r.nb1 > 0 ? r.nb0 + r.nb1 : 1;
-    const int64_t most = (bwd ? 512 : 1024) / nb > 1 ? (bwd ? 512 : 1024) / nb : 1;
-    const int64_t each = norm == 0 ? 1 : (need + most - 1) / most;
+    const int64_t all = norm == 0 ? 1 << 23 : bwd ? 512 : 1024, most = all / nb > 1 ? all / nb : 1;
+    const int64_t each = (need + most - 1) / most;
     r.gx = (unsigned)(each > 0 ? (need + each - 1) / each : 0);
     return r;
 }

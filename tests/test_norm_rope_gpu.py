@@ -152,6 +152,32 @@ def test_rope_strided():
     assert not buf[:, :, :H].any() and not buf[:, :, 2 * H:].any() and torch.equal(buf[:, :, H:2 * H], want)
 
 
+def test_rope_far_into_a_buffer():
+    """Batches more than 2^32 bytes apart; more tokens than a launch takes at one
+    per wave (2^25 + 5): the places are those of calls on slices."""
+    torch = torch_mod()
+    r = Draws(9)
+    buf = torch.empty(2 * (1 << 31) + 4096, device="cuda", dtype=torch.bfloat16)
+    x = buf.as_strided((3, 7, 2, 64), (1 << 31, 128, 64, 1))
+    dense = r(3, 7, 2, 64)
+    x.copy_(dense)
+    cos, sin = r.angles(7, 32)
+    want = torch.empty_like(dense)
+    xd.xdit_rope(dense, cos, sin, want)
+    xd.xdit_rope(x, cos, sin, x)
+    assert torch.equal(x, want)
+    N = (1 << 25) + 5
+    x = buf[:N * 64].view(1, N, 1, 64).normal_()
+    cos, sin = (torch.empty(N, 4, device="cuda").uniform_(-1, 1) for _ in range(2))
+    y = torch.full_like(x, float("nan"))
+    xd.xdit_rope(x, cos, sin, y)
+    for a, b in ((0, 1000), (N // 2 - 300, N // 2 + 300), (N - 1000, N)):
+        want = torch.empty_like(x[:, a:b])
+        xd.xdit_rope(x[:, a:b], cos[a:b], sin[a:b], want)
+        assert torch.equal(y[:, a:b], want)
+    assert not y.isnan().any()
+
+
 # -- norms --------------------------------------------------------------------
 CASES = [  # B, N, H, Hk, d, rot, weights
     (2, 37, 3, 3, 64, 64, "f32"), (1, 1, 24, 24, 128, 128, "bf16"), (2, 130, 17, 5, 72, 72, "bf16"), (1, 300, 24, 0, 128, 56, "f32"),
