@@ -163,6 +163,26 @@ def test_strongly_negative_lse():
         _check(dict(dq=dq, dk=dk, dv=dv), want, f"{dtype} d{d}")
 
 
+def test_far_into_long_tensors():
+    """Batches past 2^32 bytes of the queries' tensors, then of the keys': the
+    last one's gradients against the formulas."""
+    torch = torch_mod()
+    B, H, d = 273, 32, 128
+    for nq, nk in ((2000, 4), (4, 2000)):
+        new = lambda n: torch.zeros(B, n, H, d, device="cuda", dtype=torch.bfloat16)
+        q, k, v, out, dout = new(nq), new(nk), new(nk), new(nq), new(nq)
+        assert max(t.numel() for t in (q, k)) * 2 > 1 << 32
+        lse = torch.zeros(B, H, nq, device="cuda")
+        last = _inputs(320, 1, nq, nk, H, d, "bf16")
+        for t, s in zip((q, k, v, out, lse, dout), last):
+            t[-1:] = s
+        got = _grads(q, k)
+        xd.xdit_chunk_attn_bwd(q, k, v, out, lse, dout, *got, workspace=_ws(q, nk))
+        want = ref.attention_bwd(*(_np(t) for t in last[:6]), None, "bf16")
+        _check(dict(zip(("dq", "dk", "dv"), (t[-1:] for t in got))), want, f"{nq}x{nk}")
+        assert not any(t[:-1].any() for t in got)
+
+
 def test_empty_sides():
     torch = torch_mod()
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, device="cuda", dtype=dt)
