@@ -1,7 +1,9 @@
 /*
  * xdit.h -- C ABI of the MI355X (gfx950) DiT attention hot path of xDiT
  * (arXiv 2411.01738): the PipeFusion patch step, the sequence-parallel chunk
- * step and the log-sum-exp merge of chunk partials, as one GPU executes them.
+ * step and the log-sum-exp merge of chunk partials, as one GPU executes them;
+ * and what surrounds the attention in a layer: rotary positions, norms of
+ * queries and keys, and the gradients of these and of the chunk step.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -438,8 +440,9 @@ typedef struct {
  *   q, q_out [batch, tokens, q_heads, head_dim]
  *   k, k_out [batch, tokens, k_heads, head_dim]
  * q_out may be exactly q, and k_out exactly k (the same pointer and strides);
- * otherwise outputs overlap nothing.  Views of one fused projection, whose
- * rows interleave, count by their heads.  strides: 4 x 3 (q, k, q_out, k_out).
+ * otherwise outputs overlap nothing.  Interleaved views of one buffer (a fused
+ * projection's) count by their elements, where these keep to different parts of
+ * some stride.  strides: 4 x 3 (q, k, q_out, k_out).
  */
 int xdit_qk_norm_rope(const xdit_qk* p, const void* q, const void* k, void* q_out, void* k_out);
 

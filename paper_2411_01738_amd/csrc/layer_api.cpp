@@ -70,19 +70,30 @@ bool same_view(const View& a, const View& b) {
     return a.p == b.p && std::equal(a.n, a.n + 3, b.n) && std::equal(a.s, a.s + 3, b.s);
 }
 
-// Whether two views share no element: their spans lie apart, or both are runs
-// of heads at other places of rows that they step alike (parts of one fused
-// projection's output).
+// Length of a view's elements modulo a period, -1 where its longer strides are
+// no multiples of it.
+int64_t reach_within(const View& v, int64_t period) {
+    int64_t r = v.d;
+    for (int i = 0; i < 3; ++i) {
+        if (v.s[i] < period) r += (v.n[i] - 1) * v.s[i];
+        else if (v.s[i] % period != 0) return -1;
+    }
+    return r;
+}
+
+// Whether two views share no element: their spans lie apart, or there is a
+// stride of which their elements keep to different parts (heads of one fused
+// projection's rows, head-major tensors of one buffer, every other token).
 bool apart(const View& a, const View& b) {
     if (!overlap(a.span(), b.span())) return true;
-    const bool one_token = a.n[1] <= 1, one_batch = a.n[0] <= 1;
-    if (a.n[0] != b.n[0] || a.n[1] != b.n[1] || a.s[0] != b.s[0] || a.s[1] != b.s[1]) return false;
-    const int64_t row = one_token ? (one_batch ? 0 : a.s[0]) : a.s[1];
-    const int64_t ra = (a.n[2] - 1) * a.s[2] + a.d, rb = (b.n[2] - 1) * b.s[2] + b.d;
-    if (row <= 0 || ra > row || rb > row || (!one_batch && a.s[0] % row != 0)) return false;
     const int64_t delta = ((intptr_t)b.p - (intptr_t)a.p) / a.es;
-    const int64_t r = ((delta % row) + row) % row;
-    return r >= ra && r + rb <= row;
+    for (const View* v : {&a, &b})
+        for (const int64_t period : v->s) {
+            if (period <= 0) continue;
+            const int64_t ra = reach_within(a, period), rb = reach_within(b, period), r = (delta % period + period) % period;
+            if (ra >= 0 && rb >= 0 && r >= ra && r + rb <= period) return true;
+        }
+    return false;
 }
 
 int check_apart(const View& out, const View& in) {

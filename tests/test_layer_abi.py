@@ -13,6 +13,9 @@ from tests.test_abi import P, needs_no_gpu
 pytestmark = needs_no_gpu
 
 
+HIP = -8
+
+
 def _i32(*x):
     return (ctypes.c_int32 * len(x))(*x)
 
@@ -99,6 +102,12 @@ def test_qk_tensors():
     assert f(p, P(0), P(0) + 256, P(0) + 128, P(0) + 256) == -6
     assert f(p, P(0), P(0) + 256, P(0), P(0) + 128) == -6
     assert f(p, P(0), P(0) + 256, P(0) + 2 * row - 128, P(0) + 256) == -6   # from the last head into the next row
+    # q, k, v of [B, 3, H, N, d], of [B, N, H, 3, d], every other token; H = 2, N = 16: elements shared by one
+    for strides, ok, bad in (([3 * 2 * 16 * 64, 64, 16 * 64], 2 * 16 * 64, 2 * 16 * 64 - 64), ([16 * 6 * 64, 6 * 64, 3 * 64], 64, 3 * 64),
+                             ([32 * 2 * 64, 4 * 64, 64], 2 * 64, 64)):
+        p = _qk(strides=ctypes.cast(_i64(*strides * 4), ctypes.POINTER(ctypes.c_int64)))
+        assert f(p, P(0), P(0) + 2 * bad, P(0), P(0) + 2 * bad) == -6
+        assert f(p, P(0), P(0) + 2 * ok, P(0), P(0) + 2 * ok) == HIP   # to the launch, which has no device
     # nothing to do
     assert f(_qk(batch=0), None, None, None, None) == 0
 

@@ -281,6 +281,24 @@ def test_heads_of_zeros_and_one_value():
     assert torch.isnan(y[0, 1, 0]).all() and not torch.isnan(y[0, 1, 1]).any() and not torch.isnan(y[0, 0]).any()
 
 
+def test_views_of_one_buffer_in_place():
+    """Queries and keys that interleave by tensor, by head or by token."""
+    torch = torch_mod()
+    r = Draws(41)
+    B, N, H, d = 2, 19, 5, 64
+    w = r(d, dtype="f32")
+    cos, sin = r.angles(N, d // 2)
+    for shape, pick in [((B, 3, H, N, d), lambda t, i: t[:, i].transpose(1, 2)), ((B, N, H, 3, d), lambda t, i: t[:, :, :, i]),
+                        ((B, 3 * N, H, d), lambda t, i: t[:, i::3]), ((B, N, 3, H, d), lambda t, i: t[:, :, i]),
+                        ((N, B, 3, H, d), lambda t, i: t[:, :, i].transpose(0, 1))]:
+        buf = r(*shape)
+        q, k, v = (pick(buf, i) for i in range(3))
+        keep, want = v.clone(), [torch.empty(B, N, H, d, device="cuda", dtype=q.dtype) for _ in range(2)]
+        xd.xdit_qk_norm_rope(q.contiguous(), k.contiguous(), *want, norm="rms", wq=w, cos=cos, sin=sin)
+        xd.xdit_qk_norm_rope(q, k, q, k, norm="rms", wq=w, cos=cos, sin=sin)
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, keep), shape
+
+
 @pytest.mark.parametrize("layout", ["interleaved", "half"])
 def test_rotation_of_queries_and_keys(layout):
     """norm "none": both rotated in one call, and turned back by its gradient."""
