@@ -50,13 +50,13 @@ PEAK_HBM_GBS = 8000.0       # MI355X HBM3E (published)
 # kernel build it was taken on (sha256 prefix of the sources and their compile
 # flags); a different build reports null.
 MEASURED_TRAFFIC = {
-    ("pixart", "patch_attn"): {"bytes": (49360 + 13875) * 1024, "src": "d8ead101225fc088"},
-    ("sd3", "patch_attn"): {"bytes": (59122 + 9216) * 1024, "src": "d8ead101225fc088"},
+    ("pixart", "patch_attn"): {"bytes": (49388 + 13877) * 1024, "src": "9bef874b0a98be5b"},
+    ("sd3", "patch_attn"): {"bytes": (59088 + 9216) * 1024, "src": "9bef874b0a98be5b"},
     # the partitioned sweep and its fix-up, one launch of each per call
-    ("flux", "chunk_attn"): {"bytes": (139997 + 41225) * 1024, "src": "d8ead101225fc088"},
-    ("flux_ring", "chunk_attn"): {"bytes": (158680 + 41275) * 1024, "src": "d8ead101225fc088"},
-    ("cog", "patch_attn"): {"bytes": (259259 + 19744) * 1024, "src": "d8ead101225fc088"},
-    ("cog", "chunk_attn"): {"bytes": (133422 + 109990) * 1024, "src": "d8ead101225fc088"},
+    ("flux", "chunk_attn"): {"bytes": (139890 + 41227) * 1024, "src": "9bef874b0a98be5b"},
+    ("flux_ring", "chunk_attn"): {"bytes": (158659 + 41279) * 1024, "src": "9bef874b0a98be5b"},
+    ("cog", "patch_attn"): {"bytes": (259260 + 19744) * 1024, "src": "9bef874b0a98be5b"},
+    ("cog", "chunk_attn"): {"bytes": (133428 + 109990) * 1024, "src": "9bef874b0a98be5b"},
 }
 
 
@@ -85,15 +85,15 @@ def traffic_of(workload: str, kind: str) -> dict:
 # nothing.
 MEASURED_COUNTERS = {
     ("pixart", "patch_attn"): {"mfma_busy": 0.379, "file": "profiles/attn_patch_pixart_mfma_counters.txt",
-                               "src": "d8ead101225fc088"},
+                               "src": "9bef874b0a98be5b"},
     ("sd3", "patch_attn"): {"mfma_busy": 0.353, "file": "profiles/attn_patch_sd3_mfma_counters.txt",
-                            "src": "d8ead101225fc088"},
+                            "src": "9bef874b0a98be5b"},
     ("flux", "chunk_attn"): {"mfma_busy": 0.531, "file": "profiles/attn_chunk_flux_mfma_counters.txt",
-                             "src": "d8ead101225fc088"},
+                             "src": "9bef874b0a98be5b"},
     ("cog", "patch_attn"): {"mfma_busy": 0.406, "file": "profiles/attn_patch_cog_mfma_counters.txt",
-                            "src": "d8ead101225fc088"},
+                            "src": "9bef874b0a98be5b"},
     ("cog", "chunk_attn"): {"mfma_busy": 0.457, "file": "profiles/attn_patch_cog_mfma_counters.txt",
-                            "src": "d8ead101225fc088"},
+                            "src": "9bef874b0a98be5b"},
 }
 
 
