@@ -17,7 +17,7 @@
 // read once per token and batch of heads.  bf16, where a large copy reaches 5.1
 // TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 26 us (4.0
 // TB/s); gradients of layer norms and rotation of 17550 tokens, 48 + 48 heads of
-// 64, 130 us (5.0 TB/s); rotation of one such tensor 44 us (5.0 TB/s).
+// 64, 129 us (5.1 TB/s); rotation of one such tensor 43 us (5.1 TB/s).
 //
 // Work: a lane holds 2 V values of a head, both elements of each of its
 // pairs, so the rotation needs no other lane: the runs [2 V p, 2 V p + 2 V) for
@@ -182,19 +182,17 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
 
     for (uint32_t row = blockIdx.x * kWaves + wave; row < a.rows; row += gridDim.x * kWaves) {
         const uint32_t b = row / a.N, n = row - b * a.N;
-        float c[V], s[V];
+        // the loads of a token's angles and of a lane's heads together, as they lie in memory
+        f32x4 cv[V / 4], sv[V / 4];
 #pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            f32x4 cv = {}, sv = {};
-            if (i < turning) {
-                const int64_t at = b * a.table_batch + (int64_t)n * rp + col + i;
-                cv = *(const f32x4*)(a.cos + at);
-                sv = *(const f32x4*)(a.sin + at) * a.sgn;
+        for (int i = 0; i < V / 4; ++i) {
+            cv[i] = sv[i] = f32x4{};
+            if (4 * i < turning) {
+                const int64_t at = b * a.table_batch + (int64_t)n * rp + col + 4 * i;
+                cv[i] = *(const f32x4*)(a.cos + at);
+                sv[i] = *(const f32x4*)(a.sin + at);
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) c[i + e] = cv[e], s[i + e] = sv[e];
         }
-        // the loads of a lane's heads together, as they lie in memory
         typedef typename Run<T, V>::Raw Raw;
         Raw x[kBatch][2], g[BWD ? kBatch : 1][2];
         const char* px = sd.x + b * sd.xb + n * sd.xt;
@@ -213,6 +211,9 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
                 }
             }
         }
+        float c[V], s[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) c[i] = cv[i / 4][i % 4], s[i] = sv[i / 4][i % 4] * a.sgn;
         char* py = sd.y + b * sd.yb + n * sd.yt;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
