@@ -473,53 +473,85 @@ __device__ __forceinline__ void quarter_sincos(double f, int quarters, double* s
     *cs = (quarters + 1) & 2 ? -b : b;
 }
 
-// A thread's column is fixed: its frequency once, in quarter turns and 64 bits
-// (an angle of 10^6 in float32 is off by 0.06), then per row the product with
-// the position, its whole quarter turns taken off exactly.  Bound by 64-bit
-// arithmetic, 25 operations an angle: 131072 x 64 angles take 24 us (67 MB at 2.8
-// TB/s; the library's sincospi took 27).
+// A thread's columns are fixed: their frequencies once, a column per thread of
+// the workgroup, in quarter turns and 64 bits (an angle of 10^6 in float32 is off
+// by 0.06), then per row the products with the position, their whole quarter turns
+// taken off exactly.  Bound by stores and 64-bit arithmetic, 25 operations an
+// angle, and by the start of one round of workgroups: 131072 x 64 angles take 20 us
+// (67 MB at 3.3 TB/s; one column a thread 26; the library's sincospi took 27), 2^20
+// x 64 125 us (4.3 TB/s; 191), 32768 x 64 8.6 (9.8).
 struct TableAxes {
-    double log2_theta[4];  // of each axis, scaling included
+    double rate[4];  // of each axis: log2 of a pair's frequency over that of the pair before, scaling included
 };
-constexpr int kTableRows = 4;  // rows of a thread whose positions load together
 
+template <int V, int R>  // V columns of a thread, R rows whose positions load together
 __global__ __launch_bounds__(256) void rope_table_kernel(RopeTableParams a, TableAxes ax, int cols, int rows_per_block) {
-    const int col = threadIdx.x % cols, sub = threadIdx.x / cols;
-    if (sub >= rows_per_block) return;
-    int axis = 0, i = col;
-    while (axis + 1 < a.axes && i >= a.dims[axis] / 2) i -= a.dims[axis++] / 2;
-    double w = exp2(-2.0 * i / a.dims[axis] * ax.log2_theta[axis]);
-    if (a.scaling == 1) w /= a.factor;
-    if (a.scaling == 3) {
-        const double turns = a.orig_len * w * 0.15915494309189535;  // 1 / (2 pi)
-        const double share = fmin(1.0, fmax(0.0, (turns - a.slow) / (a.fast - a.slow)));
-        w = w * (share + (1.0 - share) / a.factor);
+    typedef float out_t __attribute__((ext_vector_type(V)));
+    __shared__ double freq[128];
+    const int col = threadIdx.x % (cols / V) * V, sub = threadIdx.x / (cols / V);
+    int axis[V];
+#pragma unroll
+    for (int v = 0, k = 0, end = a.dims[0] / 2; v < V; ++v) {
+        while (k + 1 < a.axes && col + v >= end) end += a.dims[++k] / 2;
+        axis[v] = k;
     }
-    w *= 0.6366197723675814;  // 2 / pi
     const int64_t step = (int64_t)gridDim.x * rows_per_block;
-    const int64_t first = (int64_t)blockIdx.x * rows_per_block + sub;
-    float *pc = a.cos + first * cols + col, *ps = a.sin + first * cols + col;
-    for (int64_t n0 = first; n0 < a.n; n0 += kTableRows * step) {
-        double pos[kTableRows];
+    int64_t n0 = (int64_t)blockIdx.x * rows_per_block + sub;
+    double pos[R][V];
+    auto load = [&] {
 #pragma unroll
-        for (int r = 0; r < kTableRows; ++r) {
-            const int64_t n = n0 + r * step < a.n ? n0 + r * step : n0;
-            pos[r] = a.pos_i64 ? (double)((const int64_t*)a.pos)[n * a.axes + axis]
-                               : (double)((const float*)a.pos)[n * a.axes + axis];
+        for (int r = 0; r < R; ++r) {
+            const int64_t n = n0 + r * step < a.n ? n0 + r * step : 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int64_t at = n * a.axes + axis[v];
+                if (v > 0 && axis[v] == axis[v - 1]) pos[r][v] = pos[r][v - 1];
+                else pos[r][v] = a.pos_i64 ? (double)((const int64_t*)a.pos)[at] : (double)((const float*)a.pos)[at];
+            }
         }
+    };
+    load();
+    if ((int)threadIdx.x < cols) {
+        int i = threadIdx.x, k = 0;
+        while (k + 1 < a.axes && i >= a.dims[k] / 2) i -= a.dims[k++] / 2;
+        double w = exp2(i * ax.rate[k]);
+        if (a.scaling == 1) w /= a.factor;
+        if (a.scaling == 3) {
+            const double turns = a.orig_len * w * 0.15915494309189535;  // 1 / (2 pi)
+            const double share = fmin(1.0, fmax(0.0, (turns - a.slow) / (a.fast - a.slow)));
+            w = w * (share + (1.0 - share) / a.factor);
+        }
+        freq[threadIdx.x] = w * 0.6366197723675814;  // 2 / pi
+    }
+    __syncthreads();
+    if (sub >= rows_per_block || n0 >= a.n) return;
+    double w[V];
 #pragma unroll
-        for (int r = 0; r < kTableRows; ++r) {
+    for (int v = 0; v < V; ++v) w[v] = freq[col + v];
+    float *pc = a.cos + n0 * cols + col, *ps = a.sin + n0 * cols + col;
+    for (;;) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
             if (n0 + r * step >= a.n) break;
-            double t = pos[r] * w;
-            if (fabs(t) >= 0x1p50) t = fma(-4.0, rint(0.25 * t), t);  // whole turns off, so that the sum below is exact
-            const double m = t + 0x1.8p52;  // the whole quarter turns, in the sum's low bits
-            double sn, cs;
-            quarter_sincos(t - (m - 0x1.8p52), (int)__builtin_bit_cast(uint64_t, m), &sn, &cs);
-            *pc = (float)(cs * a.magnitude);
-            *ps = (float)(sn * a.magnitude);
+            out_t c, s;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                double t = pos[r][v] * w[v];
+                if (fabs(t) >= 0x1p50) t = fma(-4.0, rint(0.25 * t), t);  // whole turns off, so that the sum below is exact
+                const double m = t + 0x1.8p52;  // the whole quarter turns, in the sum's low bits
+                double sn, cs;
+                quarter_sincos(t - (m - 0x1.8p52), (int)__builtin_bit_cast(uint64_t, m), &sn, &cs);
+                c[v] = (float)(cs * a.magnitude);
+                s[v] = (float)(sn * a.magnitude);
+            }
+            *(out_t*)pc = c;
+            *(out_t*)ps = s;
             pc += step * cols;
             ps += step * cols;
         }
+        n0 += R * step;
+        if (n0 >= a.n) break;
+        load();
     }
 }
 
@@ -547,11 +579,13 @@ hipError_t launch_rope_table(const RopeTableParams& p, hipStream_t s) {
     TableAxes ax{};
     for (int i = 0; i < p.axes; ++i) {
         const double dim = p.dims[i];
-        ax.log2_theta[i] = log2(p.theta) + (p.scaling == 2 ? dim / (dim - 2.0) * log2(p.factor) : 0.);
+        ax.rate[i] = -2. / dim * (log2(p.theta) + (p.scaling == 2 ? dim / (dim - 2.0) * log2(p.factor) : 0.));
     }
-    const int rpb = 256 / cols;
-    const int64_t need = (p.n + (int64_t)rpb * kTableRows - 1) / (rpb * kTableRows);
-    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)(need < 2048 ? need : 2048)), dim3(256), 0, s, p, ax, cols, rpb);
+    const bool wide = cols % 4 == 0;  // stores of 16 bytes
+    const int rpb = 256 / (wide ? cols / 4 : cols), rows = rpb * (wide ? 1 : 4);
+    const int64_t need = (p.n + rows - 1) / rows;
+    const dim3 grid((unsigned)(need < 2048 ? need : 2048));
+    hipLaunchKernelGGL((wide ? rope_table_kernel<4, 1> : rope_table_kernel<1, 4>), grid, dim3(256), 0, s, p, ax, cols, rpb);
     return hipGetLastError();
 }
 
