@@ -11,9 +11,11 @@
  *   least 16-byte aligned, to dense row-major storage.  The library allocates
  *   nothing and keeps no state except a per-thread stream and error message,
  *   the GEMM plans of xdit_stage_step (hipBLASLt's own memory) and the static
- *   scratch array of xdit_chunk_attn_split_noalloc.  The one exception is
- *   xdit_lse_merge's `outs` / `lses`, which are HOST arrays holding `n`
- *   device pointers.
+ *   scratch array of xdit_chunk_attn_split_noalloc.  Exceptions:
+ *   xdit_lse_merge's `outs` / `lses` are HOST arrays holding `n` device
+ *   pointers; xdit_rope's dims and strides, and xdit_qk with its strides, are
+ *   host data too; rotation and norms take strided tensors; norm weights,
+ *   their gradients and the LSE of the gradients need their type's alignment.
  * Layouts (the paper fixes none; this is the layout a QKV projection emits):
  *   activations  [B, N, H, d]  sequence-major, d contiguous (q, k, v, out,
  *                              fresh_k, fresh_v, merge partials)
