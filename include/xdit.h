@@ -13,7 +13,7 @@
  *   the GEMM plans of xdit_stage_step (hipBLASLt's own memory) and the static
  *   scratch array of xdit_chunk_attn_split_noalloc.  Exceptions:
  *   xdit_lse_merge's `outs` / `lses` are HOST arrays holding `n` device
- *   pointers; xdit_rope's dims and strides, and xdit_qk with its strides, are
+ *   pointers; dims, scaling, strides and xdit_qk of rotation and norms are
  *   host data too; rotation and norms take strided tensors; norm weights,
  *   their gradients and the LSE of the gradients need their type's alignment.
  * Layouts (the paper fixes none; this is the layout a QKV projection emits):
