@@ -15,17 +15,20 @@
 //
 // What bounds it: memory.  Each head is read and written once; the tables are
 // read once per token and batch of heads.  bf16, where a large copy reaches 5.1
-// TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 26 us (4.0
-// TB/s); gradients of layer norms and rotation of 17550 tokens, 48 + 48 heads of
-// 64, 129 us (5.1 TB/s); rotation of one such tensor 43 us (5.1 TB/s).
+// TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 24.5 us (4.3
+// TB/s; a copy of as much 21); layer norms and rotation of 17550 tokens, 48 + 48
+// heads of 64, 81 us (5.4 TB/s), their gradients 128 us (5.1 TB/s), the rotation of
+// one such tensor 43 us (5.1 TB/s).
 //
 // Work: a lane holds 2 V values of a head, both elements of each of its
 // pairs, so the rotation needs no other lane: the runs [2 V p, 2 V p + 2 V) for
 // neighbouring pairs, the runs at V p and rot / 2 + V p for pairs half a
 // rotation apart.  D / (2 V) lanes hold a head and share its sums; a wave
-// holds 64 / that many heads (7 at D = 72, one lane idle) and walks over
-// tokens with the same heads, so weights stay in registers and the angles of a
-// token are loaded once for up to kBatch heads of a lane.
+// holds 64 / that many heads (7 at D = 72, one lane idle) and loads
+// the angles of a token once for up to kBatch heads of a lane; where it takes
+// further tokens, these are of the same heads, so that weights stay in registers.
+// Weights come in wide loads: element by element they took 8 % of a long forward
+// pass.
 #include "kernels.h"
 
 #include <math.h>
@@ -105,12 +108,25 @@ __device__ __forceinline__ void store_run(char* p, const float* f) {
         *(u32x2*)p = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
     }
 }
-// V weights from element e on, of either type; `fill` where there are none
+// V weights from element e on, of either type (in wide loads where they are
+// aligned so); `fill` where there are none
 template <int V>
 __device__ __forceinline__ void load_weights(const void* w, int is_bf16, int e, float fill, float* f) {
+    const char* p = (const char*)w + (is_bf16 ? 2 : 4) * e;
+    if (w == nullptr) {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        f[i] = w == nullptr ? fill : is_bf16 ? bf16f(((const uint16_t*)w)[e + i]) : ((const float*)w)[e + i];
+        for (int i = 0; i < V; ++i) f[i] = fill;
+    } else if (((uintptr_t)w & 15) == 0) {
+        if (is_bf16) {
+            unpack<uint16_t, V>(*(const typename Run<uint16_t, V>::Raw*)p, f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) unpack<float, 4>(*(const f32x4*)(p + 4 * i), f + i);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = is_bf16 ? bf16f(((const uint16_t*)p)[i]) : ((const float*)p)[i];
+    }
 }
 
 // Sum over the L lanes of a head, the same bits in each of them.
@@ -237,7 +253,7 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
                 for (int i = 0; i < 2 * V; ++i) q = __builtin_fmaf(v[i], v[i], q);
                 q = head_sum<L>(q, lane, p);
                 // lanes without a head hold zeros: no quotient of theirs reaches a sum
-                const float r = live ? 1.f / __builtin_sqrtf(q * (1.f / D) + a.eps) : 0.f;
+                const float r = live ? rsqrtf(q * (1.f / D) + a.eps) : 0.f;
 #pragma unroll
                 for (int i = 0; i < 2 * V; ++i) v[i] *= r;
                 if constexpr (!BWD) {
@@ -340,20 +356,20 @@ struct NrGrid {
     unsigned gx;
 };
 
-// Workgroups along the tokens, a token per wave at a time.  The rotation alone
-// takes as many as there are (up to 2^31 threads: a launch holds fewer than
-// 2^32); where a norm's weights are loaded (or their gradients summed), no more
-// than run at once, with as many tokens for each.
-// Measured, us, at one round / twice that / a workgroup per 4 tokens: norms of
-// 4224 tokens, 24 + 24 heads of 128 26 / 32 / 33; 2 x 4096, 16 + 16 of 72 17 / 18
-// / 21; 17550, 48 + 48 of 64 91 / 93 / 90; gradients of the first 44 / 53 / 56, of
-// the last 134 / 144 / 194; rotation of 17550, 48 heads of 64 49 / 51 / 44.
-NrGrid nr_grid(int64_t rows, int heads0, int heads1, int G, int norm, bool bwd) {
+// Workgroups along the tokens, a token per wave at a time: forward as many as
+// there are (up to 2^31 threads: a launch holds fewer than 2^32); backward, where
+// each sums its weights' gradients, no more than run at once, with as many tokens
+// for each.  Measured, us, at one round / twice that / a workgroup per 4 tokens
+// (backward four times): norms of 4224 tokens, 24 + 24 heads of 128 24.9 / 25.9 /
+// 24.5; 2 x 4096, 16 + 16 of 72 15.8 / 15.3 / 16.4; 17550, 48 + 48 of 64 90 / 88 /
+// 81; gradients of the three 39.8 / 41.2 / 43.1, 32.3 / 29.7 / 31.3, 127 / 130 /
+// 136; rotation of 17550, 48 heads of 64 49 / 51 / 44.
+NrGrid nr_grid(int64_t rows, int heads0, int heads1, int G, bool bwd) {
     NrGrid r;
     r.nb0 = (heads0 + kBatch * G - 1) / (kBatch * G);
     r.nb1 = (heads1 + kBatch * G - 1) / (kBatch * G);
     const int64_t need = (rows + kWaves - 1) / kWaves, nb = r.nb0 + r.nb1 > 0 ? r.nb0 + r.nb1 : 1;
-    const int64_t all = norm == 0 ? 1 << 23 : bwd ? 512 : 1024, most = all / nb > 1 ? all / nb : 1;
+    const int64_t all = bwd ? 512 : 1 << 23, most = all / nb > 1 ? all / nb : 1;
     const int64_t each = (need + most - 1) / most;
     r.gx = (unsigned)(each > 0 ? (need + each - 1) / each : 0);
     return r;
@@ -394,7 +410,7 @@ hipError_t launch_any(const NormRopeParams& p, bool bwd, hipStream_t s) {
     const int V = run_of(p.D, p.bf16, p.rot, p.half);
     const int64_t es = p.bf16 ? 2 : 4;
     const int64_t rows = (int64_t)p.B * p.N;
-    const NrGrid g = nr_grid(rows, p.side[0].heads, p.side[1].heads, 64 / (p.D / (2 * V)), p.norm, bwd);
+    const NrGrid g = nr_grid(rows, p.side[0].heads, p.side[1].heads, 64 / (p.D / (2 * V)), bwd);
     const dim3 grid(g.gx, (unsigned)(g.nb0 + g.nb1));
     NrArgs a{};
     for (int i = 0; i < 2; ++i) {
@@ -565,7 +581,7 @@ int64_t norm_rope_bwd_partials(int64_t rows, int heads0, int heads1, int D, bool
     int64_t most = 0;
     for (int V : {4, 8}) {
         if (V == 8 && run_of(D, bf16, 0, 0) != 8) continue;
-        const NrGrid g = nr_grid(rows, heads0, heads1, 64 / (D / (2 * V)), 1, true);
+        const NrGrid g = nr_grid(rows, heads0, heads1, 64 / (D / (2 * V)), true);
         const int64_t n = (int64_t)2 * (g.nb0 + g.nb1) * g.gx * D;
         if (n > most) most = n;
     }

@@ -329,6 +329,52 @@ def test_no_rows():
         assert not dw.any() and not db.any()
 
 
+@pytest.mark.parametrize("layout,rot", [("interleaved", 64), ("half", 64), ("half", 40)])
+def test_weights_at_any_place(layout, rot):
+    """Weights and biases aligned to their type only: the bits of aligned ones."""
+    torch = torch_mod()
+    r = Draws(43)
+    for dtype, wt, d in [("bf16", "bf16", 64), ("bf16", "f32", 128), ("bf16", "bf16", 72), ("f32", "bf16", 64), ("f32", "f32", 72)]:
+        x, g = r(2, 11, 7, d, dtype=dtype), r(2, 11, 7, d, dtype=dtype)
+        cos, sin = r.angles(11, rot // 2)
+        w, b = r(d, dtype=wt, shift=1.0), r(d, dtype=wt)
+        kw = dict(norm="layer", cos=cos, sin=sin, layout=layout)
+
+        def outputs(w, b):
+            y, dx = torch.empty_like(x), torch.empty_like(x)
+            dw, ws = torch.empty(d, device="cuda"), torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(x, None), device="cuda", dtype=torch.uint8)
+            xd.xdit_qk_norm_rope(x, None, y, None, wq=w, bq=b, **kw)
+            xd.xdit_qk_norm_rope_bwd(x, None, g, None, dx, None, wq=w, dwq=dw, workspace=ws, **kw)
+            return y, dx, dw
+
+        want = outputs(w, b)
+        for off in (1, 2, 3, 5):
+            buf = torch.empty(2 * d + 16, device="cuda", dtype=w.dtype)
+            w2, b2 = buf[off:off + d], buf[d + 8 + off:2 * d + 8 + off]
+            w2.copy_(w)
+            b2.copy_(b)
+            for a, c in zip(outputs(w2, b2), want):
+                assert torch.equal(a, c)
+
+
+def test_no_query_heads():
+    """Keys alone, beside queries of no heads."""
+    torch = torch_mod()
+    r = Draws(44)
+    k, g, w = r(2, 9, 3, 64), r(2, 9, 3, 64), r(64, dtype="f32")
+    none = torch.empty(2, 9, 0, 64, device="cuda", dtype=k.dtype)
+    want, y = torch.empty_like(k), torch.full_like(k, float("nan"))
+    xd.xdit_qk_norm_rope(k, None, want, None, norm="rms", wq=w)
+    xd.xdit_qk_norm_rope(none, k, none, y, norm="rms", wk=w)
+    assert torch.equal(y, want)
+    dq, dk = torch.empty_like(k), torch.empty_like(k)
+    dw = [torch.full((64,), float("nan"), device="cuda") for _ in range(3)]
+    ws = torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(k, k), device="cuda", dtype=torch.uint8)
+    xd.xdit_qk_norm_rope_bwd(k, None, g, None, dq, None, norm="rms", wq=w, dwq=dw[0], workspace=ws)
+    xd.xdit_qk_norm_rope_bwd(none, k, none, g, none, dk, norm="rms", wk=w, dwq=dw[1], dwk=dw[2], workspace=ws)
+    assert torch.equal(dk, dq) and torch.equal(dw[2], dw[0]) and not dw[1].any()
+
+
 def test_many_rows_for_each_wave():
     """More tokens than waves: every row is done, and the weights' gradients
     hold them all (exactly: rows of ones and small whole gradients)."""
