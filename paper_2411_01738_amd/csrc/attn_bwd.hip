@@ -517,12 +517,34 @@ __device__ __forceinline__ void sweep(const BwdArgs& a, unsigned char* lds, int 
         }
     };
     auto result = [&](void* dst, int64_t part0, const f32x16* acc, const f32x4* tail, float f) {
+        if (a.splits == 1 && !a.accum) {
+            // stores of 16 bytes, 32 together: half hf takes both halves' dims
+            // 8 (g + hf) .. + 7 (2 x 24 heads of 64, 128 x 4429: 46 us, 51 with
+            // stores of 8 bytes; whole rows by way of LDS: the same)
 #pragma unroll
-        for (int db = 0; db < DBLK; ++db)
+            for (int db = 0; db < DBLK; ++db)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                put(dst, part0, row, 32 * db + 8 * g + 4 * hf,
-                    f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]} * f);
+                for (int g = 0; g < 4; g += 2) {
+                    u32x4 w;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int v = 4 * g + 2 * i;
+                        const auto r = __builtin_amdgcn_permlane32_swap(pack_bf16x2(acc[db][v] * f, acc[db][v + 1] * f),
+                                                                        pack_bf16x2(acc[db][v + 4] * f, acc[db][v + 5] * f), false, false);
+                        w[i] = r[0];
+                        w[2 + i] = r[1];
+                    }
+                    if (row < a.Nr)
+                        *(u32x4*)((uint16_t*)dst + ((int64_t)b * a.Nr + row) * rs + headoff + 32 * db + 8 * (g + hf)) = w;
+                }
+        } else {
+#pragma unroll
+            for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    put(dst, part0, row, 32 * db + 8 * g + 4 * hf,
+                        f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]} * f);
+        }
         if constexpr (C::TAIL)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
