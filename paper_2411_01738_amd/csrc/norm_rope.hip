@@ -15,15 +15,15 @@
 //
 // What bounds it: memory.  Each head is read and written once; the tables are
 // read once per token and batch of heads.  bf16, where a large copy reaches 5.1
-// TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 24.5 us (4.3
+// TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 23.3 us (4.5
 // TB/s; a copy of as much 21); layer norms and rotation of 17550 tokens, 48 + 48
-// heads of 64, 81 us (5.4 TB/s), their gradients 128 us (5.1 TB/s), the rotation of
+// heads of 64, 80 us (5.5 TB/s), their gradients 128 us (5.1 TB/s), the rotation of
 // one such tensor 43 us (5.1 TB/s).
 //
 // Work: a lane holds 2 V values of a head, both elements of each of its
-// pairs, so the rotation needs no other lane: the runs [2 V p, 2 V p + 2 V) for
-// neighbouring pairs, the runs at V p and rot / 2 + V p for pairs half a
-// rotation apart.  D / (2 V) lanes hold a head and share its sums; a wave
+// pairs, so the rotation needs no other lane: the runs at V p and D / 2 + V p for
+// neighbouring pairs (in one run they took 7 % more at D = 128), at V p and rot / 2
+// + V p for pairs half a rotation apart.  D / (2 V) lanes hold a head and share its sums; a wave
 // holds 64 / that many heads (7 at D = 72, one lane idle) and loads
 // the angles of a token once for up to kBatch heads of a lane; where it takes
 // further tokens, these are of the same heads, so that weights stay in registers.
@@ -40,6 +40,12 @@ namespace {
 
 constexpr int kWaves = 4;   // waves per workgroup, a token each at a time
 constexpr int kBatch = 4;   // heads of a lane per token, their loads issued together
+// Pairs of neighbours: the runs of V from V p on of both halves of the head, so
+// that a load or store of a head's lanes is one piece; at d = 72, whose V is 4, one
+// run of 2 V (the pieces would be of 8 bytes).
+template <int D>
+constexpr bool kSplit = D != 72;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct NrSide {
     const char* x;
@@ -144,15 +150,15 @@ __device__ __forceinline__ float head_sum(float v, int lane, int p) {
     }
 }
 
-// The first `turning` pairs of a lane's values rotated by (c, s): pairs of
-// neighbours, or of the runs a and b = a + V.  The others stay as they are,
-// whatever stands beside them.
+// A lane's pairs i below t1 (i < V / 2) or t2 (the others) rotated by (c, s):
+// pairs of neighbours, or of the runs a and b = a + V.  The others stay as they
+// are, whatever stands beside them.
 template <int V>
-__device__ __forceinline__ void rotate(float* x, const float* c, const float* s, int turning, bool half) {
+__device__ __forceinline__ void rotate(float* x, const float* c, const float* s, int t1, int t2, bool half) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const float a = half ? x[i] : x[2 * i], b = half ? x[V + i] : x[2 * i + 1];
-        const bool on = i < turning;
+        const bool on = i < (i < V / 2 ? t1 : t2);
         const float ya = on ? a * c[i] - b * s[i] : a, yb = on ? b * c[i] + a * s[i] : b;
         if (half) {
             x[i] = ya;
@@ -174,14 +180,17 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
     const int head0 = ((int)blockIdx.y - (second ? a.nb0 : 0)) * kBatch * G + grp;
     const int rp = a.rot / 2;
 
-    // this lane's two runs of V elements, and the pair that the first belongs to
+    // this lane's two runs of V elements; its pair i is that of number p1 + i (i <
+    // V / 2) or p2 + i, and turns if i is below t1 or t2 (steps of V / 2 pairs)
+    constexpr bool SPLIT = !HALF && kSplit<D>;
     const int col = V * p;
-    int oa = 2 * V * p, ob = oa + V;
+    int oa = SPLIT ? col : 2 * col, ob = SPLIT ? D / 2 + col : oa + V;
     if (HALF) {
         if (col < rp) oa = col, ob = rp + col;
         else oa = a.rot + 2 * (col - rp), ob = oa + V;
     }
-    const int turning = rp - col;  // pairs of this lane that rotate (a multiple of 4, or none)
+    const int p1 = SPLIT ? col / 2 : col, p2 = SPLIT ? D / 4 + col / 2 - V / 2 : col;
+    const int t1 = rp - p1, t2 = rp - p2;
     float w[2 * V], bias[2 * V];
     if constexpr (NORM != 0) {
         load_weights<V>(sd.w, a.weight_bf16, oa, 1.f, w);
@@ -203,10 +212,19 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
 #pragma unroll
         for (int i = 0; i < V / 4; ++i) {
             cv[i] = sv[i] = f32x4{};
-            if (4 * i < turning) {
-                const int64_t at = b * a.table_batch + (int64_t)n * rp + col + 4 * i;
-                cv[i] = *(const f32x4*)(a.cos + at);
-                sv[i] = *(const f32x4*)(a.sin + at);
+            const int64_t at = b * a.table_batch + (int64_t)n * rp + 4 * i;
+            if constexpr (SPLIT && V == 4) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (2 * h < (h == 0 ? t1 : t2)) {
+                        const f32x2 cc = *(const f32x2*)(a.cos + at + (h == 0 ? p1 : p2) + 2 * h);
+                        const f32x2 ss = *(const f32x2*)(a.sin + at + (h == 0 ? p1 : p2) + 2 * h);
+                        cv[i][2 * h] = cc[0], cv[i][2 * h + 1] = cc[1];
+                        sv[i][2 * h] = ss[0], sv[i][2 * h + 1] = ss[1];
+                    }
+            } else if (4 * i < (4 * i < V / 2 ? t1 : t2)) {
+                cv[i] = *(const f32x4*)(a.cos + at + (4 * i < V / 2 ? p1 : p2));
+                sv[i] = *(const f32x4*)(a.sin + at + (4 * i < V / 2 ? p1 : p2));
             }
         }
         typedef typename Run<T, V>::Raw Raw;
@@ -263,7 +281,7 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
                     float gv[2 * V];
                     unpack<T, V>(g[u][0], gv);
                     unpack<T, V>(g[u][1], gv + V);
-                    rotate<V>(gv, c, s, turning, HALF);
+                    rotate<V>(gv, c, s, t1, t2, HALF);
                     float m1 = 0.f, m2 = 0.f;
 #pragma unroll
                     for (int i = 0; i < 2 * V; ++i) {
@@ -279,7 +297,7 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
                     for (int i = 0; i < 2 * V; ++i) v[i] = r * (gv[i] - __builtin_fmaf(v[i], m1, m2));
                 }
             }
-            if constexpr (!BWD) rotate<V>(v, c, s, turning, HALF);
+            if constexpr (!BWD) rotate<V>(v, c, s, t1, t2, HALF);
             if (live) {
                 store_run<T, V>(py + h * sd.yh + ES * oa, v);
                 store_run<T, V>(py + h * sd.yh + ES * ob, v + V);
@@ -304,7 +322,7 @@ __global__ __launch_bounds__(64 * kWaves) void norm_rope_kernel(NrArgs a) {
                 float sum = 0.f;
                 for (int j = 0; j < kWaves * G; ++j)
                     sum += red[((j / G) * 64 + (j % G) * L + tp) * 2 * V + ti];
-                int e = 2 * V * tp + ti;
+                int e = SPLIT ? V * tp + ti + (ti < V ? 0 : D / 2 - V) : 2 * V * tp + ti;
                 if (HALF) {
                     const int tc = V * tp;
                     if (tc < rp) e = (ti < V ? tc : rp + tc - V) + ti;
