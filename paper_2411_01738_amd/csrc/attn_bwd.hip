@@ -12,7 +12,7 @@
 // queries x keys is stored.  P and dS are rounded to bf16 as operands of the
 // matrix cores (half a step, 2^-8 relative, each; the sums are float32).
 //
-// What bounds it: the matrix cores (24 heads of 128, 4224 x 4224: 690 us, 1110
+// What bounds it: the matrix cores (24 heads of 128, 4224 x 4224: 683 us, 1120
 // TFLOP/s over the seven products, where a large product of random values
 // reaches 1372).  One sweep gives dK and dV (four products
 // of queries x keys x d), another dQ (three), seven in place of the five that
@@ -699,7 +699,8 @@ hipError_t launch_sweeps(const BwdArgs& kv, const BwdArgs& q, hipStream_t s) {
 // and most of one of the shorter ones, which come last, or as long as the
 // longest.  Cut sweeps add the join: a launch, and partials written and read at
 // 2 TB/s.
-// Measured in one part, and in the best, us: 2 x 16 heads of 72, 1024 x 1024 45
+// Measured in one part, and in the best, us (with results in stores of 8 bytes,
+// 2 to 10 % more than now): 2 x 16 heads of 72, 1024 x 1024 45
 // (dQ in 2: 49); 24 heads of 128, 512 x 4224 117, dQ in 2 107; 2 x 24 heads of
 // 64, 333 x 4429 88; 24 heads of 64, 1 x 4429 55, dQ in 4 27; 24 heads of 128,
 // 4224 x 64 132, dK/dV in 6 47; 3 heads of 128, 4224 x 4224 130, dQ in 2 and

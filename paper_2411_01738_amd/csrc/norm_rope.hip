@@ -22,13 +22,13 @@
 //
 // Work: a lane holds 2 V values of a head, both elements of each of its
 // pairs, so the rotation needs no other lane: the runs at V p and D / 2 + V p for
-// neighbouring pairs (in one run they took 7 % more at D = 128), at V p and rot / 2
-// + V p for pairs half a rotation apart.  D / (2 V) lanes hold a head and share its sums; a wave
-// holds 64 / that many heads (7 at D = 72, one lane idle) and loads
-// the angles of a token once for up to kBatch heads of a lane; where it takes
-// further tokens, these are of the same heads, so that weights stay in registers.
-// Weights come in wide loads: element by element they took 8 % of a long forward
-// pass.
+// neighbouring pairs (in one run they took 7 % more at D = 128), at V p and
+// rot / 2 + V p for pairs half a rotation apart.  D / (2 V) lanes hold a head and
+// share its sums; a wave holds 64 / that many heads (7 at D = 72, one lane idle)
+// and loads the angles of a token once for up to kBatch heads of a lane; where it
+// takes further tokens, these are of the same heads, so that weights stay in
+// registers.  Weights come in wide loads: element by element they took 8 % of a
+// long forward pass.
 #include "kernels.h"
 
 #include <math.h>
