@@ -699,14 +699,13 @@ hipError_t launch_sweeps(const BwdArgs& kv, const BwdArgs& q, hipStream_t s) {
 // and most of one of the shorter ones, which come last, or as long as the
 // longest.  Cut sweeps add the join: a launch, and partials written and read at
 // 2 TB/s.
-// Measured in one part, and in the best, us (with results in stores of 8 bytes,
-// 2 to 10 % more than now): 2 x 16 heads of 72, 1024 x 1024 45
-// (dQ in 2: 49); 24 heads of 128, 512 x 4224 117, dQ in 2 107; 2 x 24 heads of
-// 64, 333 x 4429 88; 24 heads of 64, 1 x 4429 55, dQ in 4 27; 24 heads of 128,
-// 4224 x 64 132, dK/dV in 6 47; 3 heads of 128, 4224 x 4224 130, dQ in 2 and
-// dK/dV in 3 103; one head of 64, 8000 x 8000 121, dQ in 4 and dK/dV in 4 66;
+// Measured in one part, and in the best, us: 2 x 16 heads of 72, 1024 x 1024 47
+// (dQ in 2: 56); 24 heads of 128, 512 x 4224 114, dQ in 2 104; 2 x 24 heads of
+// 64, 333 x 4429 84; 24 heads of 64, 1 x 4429 53, dQ in 4 24; 24 heads of 128,
+// 4224 x 64 129, dK/dV in 8 45; 3 heads of 128, 4224 x 4224 125, dQ in 3 and
+// dK/dV in 2 104; one head of 64, 8000 x 8000 116, dQ in 4 and dK/dV in 4 67;
 // float32, 2 heads of 64, 256 x 64 25, dQ in 2 and dK/dV in 8 13.  Over 86 calls
-// timed with all parts, the model's choice takes 2.6 % more time than the best in
+// timed with all parts, the model's choice takes 1.9 % more time than the best in
 // the mean, at worst 33 %.
 BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16) {
     BwdSplits best{1, 1, bf16 ? kRows : 64};
