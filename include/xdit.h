@@ -365,8 +365,9 @@ int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void*
  * (text, height and width of an image, time of a video); axis a turns
  * dims[a] / 2 pairs, the axes' pairs one after another:
  *   angle = position * w,  w = theta^(-2 i / dims[a]),  i = 0 .. dims[a]/2 - 1
- * Angles are formed and reduced in 64 bits: an angle of size a is off by about
- * a * 2^-52 before the table is rounded to float32.
+ * Angles are formed and reduced in 64 bits: an angle of size a is off by at most
+ * 4 a * 2^-52 (on the slope of a ramp about three times that) before the table is
+ * rounded to float32.
  *   pos      [n, n_axes]  int64 (XDIT_I64) or float32 (XDIT_F32: fractional
  *                         positions of a grid that is stretched or cropped)
  *   dims     HOST array of n_axes even positive numbers, at most 256 in all

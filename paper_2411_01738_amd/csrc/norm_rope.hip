@@ -514,8 +514,13 @@ __device__ __forceinline__ void quarter_sincos(double f, int quarters, double* s
 // angle, and by the start of one round of workgroups: 131072 x 64 angles take 20 us
 // (67 MB at 3.3 TB/s; one column a thread 26; the library's sincospi took 27), 2^20
 // x 64 125 us (4.3 TB/s; 191), 32768 x 64 8.6 (9.8).
+//
+// Frequencies are 2^(i rate): the rounding of an exponent of size e would be
+// one of e ln 2 / 2 steps in the frequency (up to 7 measured at dims of 72, theta
+// 10^4), so the rate comes in two parts, and what the product of its first part
+// and i rounds away goes into the result to first order.
 struct TableAxes {
-    double rate[4];  // of each axis: log2 of a pair's frequency over that of the pair before, scaling included
+    double rate[4], rest[4];  // of each axis: log2 of a pair's frequency over that of the pair before, scaling included
 };
 
 template <int V, int R>  // V columns of a thread, R rows whose positions load together
@@ -548,7 +553,9 @@ __global__ __launch_bounds__(256) void rope_table_kernel(RopeTableParams a, Tabl
     if ((int)threadIdx.x < cols) {
         int i = threadIdx.x, k = 0;
         while (k + 1 < a.axes && i >= a.dims[k] / 2) i -= a.dims[k++] / 2;
-        double w = exp2(i * ax.rate[k]);
+        const double e = i * ax.rate[k];
+        double w = exp2(e);
+        w = fma(w, 0.6931471805599453 * fma((double)i, ax.rest[k], fma((double)i, ax.rate[k], -e)), w);
         if (a.scaling == 1) w /= a.factor;
         if (a.scaling == 3) {
             const double turns = a.orig_len * w * 0.15915494309189535;  // 1 / (2 pi)
@@ -612,8 +619,10 @@ hipError_t launch_rope_table(const RopeTableParams& p, hipStream_t s) {
     if (p.n == 0) return hipSuccess;
     TableAxes ax{};
     for (int i = 0; i < p.axes; ++i) {
-        const double dim = p.dims[i];
-        ax.rate[i] = -2. / dim * (log2(p.theta) + (p.scaling == 2 ? dim / (dim - 2.0) * log2(p.factor) : 0.));
+        const long double dim = p.dims[i];
+        const long double rate = -2 * (log2l(p.theta) + (p.scaling == 2 ? dim / (dim - 2) * log2l(p.factor) : 0)) / dim;
+        ax.rate[i] = (double)rate;
+        ax.rest[i] = (double)(rate - ax.rate[i]);
     }
     const bool wide = cols % 4 == 0;  // stores of 16 bytes
     const int rpb = 256 / (wide ? cols / 4 : cols), rows = rpb * (wide ? 1 : 4);

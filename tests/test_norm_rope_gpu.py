@@ -89,6 +89,49 @@ def test_far_positions_stay_on_the_circle():
     assert ((cos[2:].double() ** 2 + sin[2:].double() ** 2 - 1).abs() < 1e-6).all()
 
 
+@pytest.mark.parametrize("dims,kw", [
+    ([128], {}), ([72], {}), ([24, 40], {}), ([64], dict(theta=500000.0)), ([72], dict(theta=500000.0, scaling="linear", factor=3.7)),
+    ([72], dict(scaling="ntk", factor=3.7)), ([256], dict(scaling="ntk", factor=2.0)),
+    ([128], dict(scaling="ramp", factor=3.0, orig_len=4096))])
+def test_table_error_by_angle(dims, kw):
+    """Every column's error against the size of its own angle, at positions so
+    far (2^36) that it stands above the table's rounding: 4 * 2^-52 of the angle
+    (the power is good to one and its correction to half a step, the quotient
+    by the factor, the constant 2 / pi, the product with it and the one with the
+    position to half a step each).  On the slope of a ramp 12: the turns within the original length are
+    good to 3 steps, the share to 1.5 more, of which the frequency takes at most
+    (3 * 3 * slow / (fast - slow) + 4.5), its own sum 1.5, and the steps from
+    before and after it 4.  The angles are formed in 80 bits."""
+    torch = torch_mod()
+    n = 700
+    g = torch.Generator().manual_seed(21)
+    pos = torch.randint(0, 1 << 30, (n, len(dims)), generator=g) + (1 << 36)
+    cos, sin = (torch.full((n, sum(dims) // 2), float("nan"), device="cuda") for _ in range(2))
+    xd.xdit_rope_table(pos.cuda(), dims, cos, sin, **kw)
+    L = np.longdouble
+    if np.finfo(L).nmant < 63:
+        pytest.skip("no 80-bit numbers")
+    cols = []
+    for a, dim in enumerate(dims):
+        th, f, kind = L(kw.get("theta", 10000.0)), L(kw.get("factor", 1.0)), kw.get("scaling", "none")
+        if kind == "ntk":
+            th = th * f ** (L(dim) / L(dim - 2))
+        w = np.exp2(-2 * np.arange(dim // 2).astype(L) / L(dim) * np.log2(th))
+        if kind == "linear":
+            w = w / f
+        elif kind == "ramp":
+            t = (kw["orig_len"] * w / (2 * np.arctan2(L(0), L(-1))) - 1) / L(31)
+            t = np.clip(t, 0, 1)
+            w = w * t + w / f * (1 - t)
+        cols.append(pos[:, a].numpy().astype(L)[:, None] * w)
+    ang = np.concatenate(cols, 1)
+    steps = 12 if kw.get("scaling") == "ramp" else 4
+    for got, want, what in ((cos, np.cos(ang), "cos"), (sin, np.sin(ang), "sin")):
+        err = np.abs(got.cpu().numpy().astype(L) - want)
+        over = err - (L(2) ** -24 * np.abs(want) + steps * L(2) ** -52 * ang + 1e-12)
+        assert (over <= 0).all(), f"{what}: column {int(over.max(0).argmax())} off by {float(err.max()):.3e}"
+
+
 def test_table_of_no_rows():
     torch = torch_mod()
     e = torch.empty(0, 32, device="cuda")
