@@ -340,6 +340,8 @@ def xdit_stage_step(x, wq, wk, wv, wo, kv_buf, patch_off: int, q, k, v, o, y, *,
     With a norm or a rotary table, q and k are normalised and rotated as by
     xdit_qk_norm_rope between the projections and the patch step: cos, sin
     hold the patch's rows, [L, r] or [B, L, r]."""
+    _choice(NORMS, "norm", norm)
+    _choice(LAYOUTS, "layout", layout)
     _buffer(kv_buf)
     _, B, N, H, d = kv_buf.shape
     _dense(x, "x", 3)

@@ -186,3 +186,13 @@ def test_stage_step_qk():
     assert f(_qk(**good, norm=0)) == -4 and f(_qk(**good, rot_dim=12)) == -3
     assert f(_qk(**good, cos=P(9))) == -6 and f(_qk(**good, wq=P(5))) == -6 and f(_qk(**good, wk=P(6))) == -6
     assert f(_qk(**good), q=P(6), k=P(6)) == -6 and f(_qk(**good), dtype=1) == -7
+
+
+@pytest.mark.parametrize("bad", [dict(layout="other"), dict(layout=0), dict(norm="other"), dict(norm=None)])
+def test_stage_step_names(bad):
+    """A wrong name is refused before anything else, also where nothing is
+    rotated or normalised."""
+    import paper_2411_01738_amd as xd
+
+    with pytest.raises(xd.XditError, match=f"{list(bad)[0]} = "):
+        xd.xdit_stage_step(None, None, None, None, None, None, 0, None, None, None, None, None, **bad)
