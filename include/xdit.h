@@ -346,11 +346,12 @@ int xdit_stage_step(const void* x, const void* wq, const void* wk, const void* w
  *   workspace    xdit_chunk_attn_bwd_workspace_bytes(...) bytes, 256-byte
  *                aligned, overlapping nothing; its contents on entry do not
  *                matter.  Calls that overlap in time need one each.
- * A row whose lse is -inf (it met no key) has no part in any gradient; its out
- * is not read, its dout must be finite.  kv_len = 0 gives dq = 0, q_len = 0
- * gives dk = dv = 0.  Sums are float32 and their order is fixed: the same call
- * gives the same bits.  bf16 calls round P and the scores' gradient to bf16 as
- * operands of the matrix cores.  No output overlaps another tensor.
+ * A row whose lse is -inf (it met no key) has no part in any gradient.  Its out
+ * and dlse may hold anything; its q and dout are multiplied by zeros, so they
+ * must be finite, and their products with k and v too.  kv_len = 0 gives dq = 0,
+ * q_len = 0 gives dk = dv = 0.  Sums are float32 and their order is fixed: the
+ * same call gives the same bits.  bf16 calls round P and the scores' gradient to
+ * bf16 as operands of the matrix cores.  No output overlaps another tensor.
  */
 int64_t xdit_chunk_attn_bwd_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads,
                                             int64_t head_dim, int32_t dtype);

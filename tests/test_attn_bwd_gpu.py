@@ -143,6 +143,26 @@ def test_rows_without_keys():
         assert not dq.any() and not dk.any() and not dv.any()
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 72), ("bf16", 128), ("f32", 64)])
+def test_rows_without_keys_hold_anything_finite(dtype, d):
+    """Their out and dlse are NaN, their q and dout far above the others'."""
+    nq, nk = 140, 70
+    q, k, v, out, lse, dout, e = _inputs(311, 1, nq, nk, 2, d, dtype, dlse=True)
+    dead = torch_mod().zeros(1, 2, nq, dtype=torch_mod().bool, device="cuda")
+    dead[:, 0, 1::3] = True
+    dead[:, 1, 90:] = True
+    rows = dead.transpose(1, 2)
+    lse[dead], e[dead], out[rows], q[rows], dout[rows] = float("-inf"), float("nan"), float("nan"), 1e15, -1e15
+    dq, dk, dv = _grads(q, k)
+    xd.xdit_chunk_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, dlse=e, workspace=_ws(q, nk))
+    assert not dq[rows].any()
+    # for the formulas and their error the rows are rows of zeros
+    for t in (out, q, dout):
+        t[rows] = 0.0
+    want = ref.attention_bwd(_np(q), _np(k), _np(v), _np(out), _np(lse), _np(dout), np.nan_to_num(_np(e)), dtype)
+    _check(dict(dq=dq, dk=dk, dv=dv), want, dtype)
+
+
 def test_strongly_negative_lse():
     """Rows whose scores lie far below zero: padding keys of a tile, whose score
     would be zero, must not reach them."""
