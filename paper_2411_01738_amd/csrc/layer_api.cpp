@@ -181,7 +181,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // launch, and few resident rows over a long other side would leave CUs idle.
 struct BwdPlan {
     int q_splits, kv_splits;
-    int64_t q_wgs, kv_wgs;            // workgroups of a batch and head
+    int64_t step;                        // batches of a launch
     int64_t rows_bytes, q_bytes, bytes;  // of the workspace: the rows' scalars, the partials of dq, of dk and dv
 };
 
@@ -189,10 +189,14 @@ BwdPlan bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t d, int32_
     BwdPlan p;
     const xdit::BwdSplits s = xdit::bwd_splits(B * H, Nq, Nk, (int)d, dtype == XDIT_BF16);
     p.q_splits = s.q, p.kv_splits = s.kv;
-    p.q_wgs = ceil_div(Nq, s.rows) * s.q, p.kv_wgs = ceil_div(Nk, s.rows) * s.kv;
-    p.rows_bytes = align256(8 * B * H * Nq);
-    p.q_bytes = p.q_splits > 1 ? align256(4 * p.q_splits * B * Nq * H * d) : 0;
-    p.bytes = p.rows_bytes + p.q_bytes + (p.kv_splits > 1 ? align256(8 * p.kv_splits * B * Nk * H * d) : 0);
+    // a grid holds fewer than 2^32 threads: whole batches at a time, which use
+    // the workspace one after another
+    const int64_t sweeps = ceil_div(Nq, s.rows) * s.q + ceil_div(Nk, s.rows) * s.kv;
+    const int64_t wgs = std::max<int64_t>(1, H * std::max(ceil_div(Nq, 8), sweeps));
+    p.step = std::min(B, std::max<int64_t>(1, (((int64_t)1 << 24) - 1) / wgs));
+    p.rows_bytes = align256(8 * p.step * H * Nq);
+    p.q_bytes = p.q_splits > 1 ? align256(4 * p.q_splits * p.step * Nq * H * d) : 0;
+    p.bytes = p.rows_bytes + p.q_bytes + (p.kv_splits > 1 ? align256(8 * p.kv_splits * p.step * Nk * H * d) : 0);
     return p;
 }
 
@@ -472,10 +476,7 @@ int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void*
         for (int j = 0; j < i; ++j) XDIT_TRY(check_no_overlap(*outs[i], *outs[j]));
     }
     if (batch == 0 || heads == 0) return XDIT_OK;
-    // a grid holds fewer than 2^32 threads: whole batches at a time
-    const int64_t wgs = heads * std::max<int64_t>(1, std::max(ceil_div(q_len, 8), plan.q_wgs + plan.kv_wgs));
-    const int64_t step = std::max<int64_t>(1, (((int64_t)1 << 24) - 1) / wgs);
-    for (int64_t b0 = 0; b0 < batch; b0 += step) {
+    for (int64_t b0 = 0; b0 < batch; b0 += plan.step) {
         auto at = [&](const void* p, int64_t rows, int bytes) -> char* {
             return p ? (char*)const_cast<void*>(p) + b0 * rows * heads * bytes : nullptr;
         };
@@ -485,7 +486,7 @@ int xdit_chunk_attn_bwd(const void* q, const void* k, const void* v, const void*
         p.out = at(out, q_len, es * d), p.dout = at(dout, q_len, es * d);
         p.lse = (const float*)at(lse, q_len, 4), p.dlse = (const float*)at(dlse, q_len, 4);
         p.dq = at(dq, q_len, eq * d), p.dk = at(dk, kv_len, ek * d), p.dv = at(dv, kv_len, ek * d);
-        p.B = (int)std::min(step, batch - b0), p.H = (int)heads, p.Nq = (int)q_len, p.Nk = (int)kv_len, p.D = d;
+        p.B = (int)std::min(plan.step, batch - b0), p.H = (int)heads, p.Nq = (int)q_len, p.Nk = (int)kv_len, p.D = d;
         p.bf16 = dtype == XDIT_BF16;
         p.accum_q = (accum & XDIT_ACCUM_DQ) != 0, p.accum_kv = (accum & XDIT_ACCUM_DKV) != 0;
         p.q_splits = plan.q_splits, p.kv_splits = plan.kv_splits;

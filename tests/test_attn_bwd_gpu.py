@@ -203,6 +203,38 @@ def test_far_into_long_tensors():
         assert not any(t[:-1].any() for t in got)
 
 
+@pytest.mark.parametrize("accum", [False, True])
+def test_several_launches(accum):
+    """More workgroups than a launch holds: batches go out in three parts (16
+    heads of one query and one key: 524287 batches at a time), with the bits of
+    a call for each part, and the formulas at the parts' borders."""
+    torch = torch_mod()
+    step, H, d = 524287, 16, 64
+    B = 2 * step + 3
+    g = torch.Generator(device="cuda").manual_seed(325)
+    f32 = torch.float32
+    new = lambda dt: torch.randn(B, 1, H, d, generator=g, device="cuda", dtype=torch.bfloat16).to(dt)
+    q, k, v, out, dout = (new(torch.bfloat16) for _ in range(5))
+    lse, dlse = (torch.randn(B, H, 1, generator=g, device="cuda") for _ in range(2))
+    lse = ((q.float() * k.float()).sum(-1).transpose(1, 2) * d ** -0.5 + lse.abs()).contiguous()
+    base = [torch.ones(B, 1, H, d, device="cuda", dtype=f32) if accum else torch.full_like(q, float("nan")) for _ in range(3)]
+    kw = dict(accum_dq=accum, accum_dkv=accum)
+    got = [t.clone() for t in base]
+    xd.xdit_chunk_attn_bwd(q, k, v, out, lse, dout, *got, dlse=dlse, workspace=_ws(q, 1), **kw)
+    for a, b in ((0, step), (step, 2 * step), (2 * step, B)):
+        part = [t[a:b].clone() for t in base]
+        xd.xdit_chunk_attn_bwd(*(t[a:b] for t in (q, k, v, out, lse, dout)), *part, dlse=dlse[a:b], workspace=_ws(q[a:b], 1), **kw)
+        for x, y in zip(got, part):
+            assert torch.equal(x[a:b], y), f"batches {a}.."
+    for a in (0, step - 1, 2 * step - 1, B - 2):
+        args = [_np(t[a:a + 2]) for t in (q, k, v, out, lse, dout, dlse)]
+        want = ref.attention_bwd(*args, "bf16")
+        grads = [t[a:a + 2] - 1.0 if accum else t[a:a + 2] for t in got]
+        if accum:  # the sum with 1 and the difference round once each
+            want = {n: (w, *(x + 2.0 ** -24 * (1 + 2 * np.abs(w)) for x in bounds)) for n, (w, *bounds) in want.items()}
+        _check(dict(zip(("dq", "dk", "dv"), grads)), want, f"batches {a}..")
+
+
 def test_empty_sides():
     torch = torch_mod()
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, device="cuda", dtype=dt)

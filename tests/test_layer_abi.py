@@ -170,6 +170,18 @@ def test_workspace_of_the_attention_gradients():
     assert f(1, 10, 10, 2, 96, 0) == -1 and f(1, -1, 10, 2, 64, 0) == -1
 
 
+def test_workspace_of_many_batches():
+    """A call of more than 2^24 - 1 workgroups runs as several launches of whole
+    batches, which share the workspace: it holds those of one.  16 heads of one
+    query and one key are 32 workgroups, so 524287 batches at a time."""
+    f = _lib.lib().xdit_chunk_attn_bwd_workspace_bytes
+    one = f(524287, 1, 1, 16, 64, 0)
+    assert 8 * 16 * 524287 <= one < 8 * 16 * 524287 + 256
+    for B in (524288, 2 * 524287 + 3):
+        assert f(B, 1, 1, 16, 64, 0) == one
+    assert f(524286, 1, 1, 16, 64, 0) < one
+
+
 def test_stage_step_qk():
     L = _lib.lib()
 
