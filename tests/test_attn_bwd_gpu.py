@@ -85,6 +85,47 @@ def test_long_sweeps_of_few_rows(dtype, d, B, H, nq, nk):
     _run(200, B, nq, nk, H, d, dtype, dlse=True)
 
 
+def _sampled(seed, B, nq, nk, H, d, dtype, heads, dlse):
+    """A call on the forward kernels' out and lse; some of its heads against the
+    formulas."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda n: torch.randn(B, n, H, d, generator=g, device="cuda").to(tdtype(dtype))
+    q, k, v, dout = r(nq), r(nk), r(nk), r(nq)
+    out, lse = torch.empty_like(q), torch.empty(B, H, nq, device="cuda")
+    xd.xdit_chunk_attn(q, k, v, out, lse)
+    e = torch.randn(B, H, nq, generator=g, device="cuda") if dlse else None
+    dq, dk, dv = _grads(q, k)
+    ws = _ws(q, nk)
+    xd.xdit_chunk_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, dlse=e, workspace=ws)
+    assert all(torch.isfinite(t).all() for t in (dq, dk, dv))
+    for b, h in heads:
+        at = lambda t: _np(t[b:b + 1, :, h:h + 1])
+        row = lambda t: None if t is None else _np(t[b:b + 1, h:h + 1])
+        want = ref.attention_bwd(at(q), at(k), at(v), at(out), row(lse), at(dout), row(e), dtype)
+        _check(dict(dq=dq[b:b + 1, :, h:h + 1], dk=dk[b:b + 1, :, h:h + 1], dv=dv[b:b + 1, :, h:h + 1]), want,
+               f"{dtype} {B}x{H} {nq}x{nk} d{d} head {b},{h}")
+    return ws.numel()
+
+
+# tiles of 64 streamed rows at bf16 head dims 64 and 72, of 32 otherwise: 11 and
+# more in both sweeps of every call, in one round of workgroups and in several
+@pytest.mark.parametrize("dtype,B,H,nq,nk", [("bf16", 1, 16, 715, 1030), ("bf16", 3, 16, 1100, 700), ("f32", 1, 16, 330, 450),
+                                             ("f32", 2, 32, 410, 345)])
+@pytest.mark.parametrize("d", [64, 72, 128])
+def test_long_sweeps_of_many_rows(dtype, B, H, nq, nk, d):
+    ws = _sampled(205, B, nq, nk, H, d, dtype, [(0, 0), (0, 7), (B - 1, H - 1)], dlse=B != 2)
+    # nothing beyond two float32 per query row: no partials, so no sweep was cut
+    assert ws == (8 * B * H * nq + 255) // 256 * 256
+
+
+@pytest.mark.parametrize("dtype,B,H,nq,nk,d", [("bf16", 2, 24, 4429, 4429, 64), ("bf16", 2, 16, 4096, 4096, 72),
+                                               ("bf16", 1, 24, 4224, 4224, 128), ("f32", 2, 16, 1024, 1024, 72)])
+def test_whole_sequences(dtype, B, H, nq, nk, d):
+    """The joint sequence of SD3, Pixart's, one chunk of Flux, a float32 share."""
+    _sampled(206, B, nq, nk, H, d, dtype, [(B - 1, 5)], dlse=False)
+
+
 @pytest.mark.parametrize("d", [64, 72, 128])
 def test_many_heads(d):
     _run(210, 2, 150, 170, 17, d, "bf16")
