@@ -305,6 +305,31 @@ def test_norm_rope_bwd(dtype, norm, layout, fused):
         assert torch.equal(gq, dq) and (gk is None or torch.equal(gk, dk)), case
 
 
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("dtype,d,rot", [("bf16", 64, 64), ("bf16", 72, 24), ("bf16", 128, 72), ("f32", 64, 16), ("f32", 128, 128)])
+def test_a_table_per_batch(dtype, d, rot, norm, layout):
+    """Each batch's own angles, forward and backward, against the formulas."""
+    torch = torch_mod()
+    r = Draws(16)
+    for B, N, H, Hk in ((3, 29, 5, 2), (2, 1, 24, 24), (4, 150, 3, 0)):
+        q, k, w, _, _ = _case(r, B, N, H, Hk, d, 0, "f32", norm, dtype, False)
+        cos, sin = r.angles(B, N, rot // 2)
+        new = lambda t: None if t is None else torch.full(t.shape, float("nan"), device="cuda", dtype=t.dtype)
+        kw = dict(norm=norm, eps=1e-5, cos=cos, sin=sin, layout=layout)
+        qo, ko, dq, dk = new(q), new(k), new(q), new(k)
+        gq, gk = r(B, N, H, d, dtype=dtype), r(B, N, Hk, d, dtype=dtype) if Hk else None
+        xd.xdit_qk_norm_rope(q, k, qo, ko, **kw, **w)
+        xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, dq, dk, wq=w["wq"], wk=w["wk"], **kw)
+        for x, y, g, dx, n in ((q, qo, gq, dq, "q"), (k, ko, gk, dk, "k")):
+            if x is None:
+                continue
+            X, W, b, c, s = _np(x), _np(w["w" + n]), _np(w["b" + n]), _np32(cos), _np32(sin)
+            _close(_np(y), ref.forward(X, W, b, c, s, norm, 1e-5, layout), ref.forward_scale(X, W, b, norm, 1e-5), dtype, n)
+            want, _, _, scale = ref.backward(X, W, _np(g), c, s, norm, 1e-5, layout)
+            _close(_np(dx), want, scale, dtype, f"d{n}")
+
+
 def test_heads_of_zeros_and_one_value():
     """A head of zeros stays zero (eps alone is under the root) and its gradient
     is finite; a head of one repeated value is what each norm makes of it."""

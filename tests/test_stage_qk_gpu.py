@@ -71,6 +71,37 @@ def test_stage_step_qk(B, L, N, H, d, C, off, norm, rot, layout):
         assert np.sqrt((err ** 2).mean()) <= 2.0 ** -7 * np.sqrt((want ** 2).mean())
 
 
+@pytest.mark.parametrize("norm,layout", [("rms", "interleaved"), ("layer", "half"), ("none", "half")])
+def test_a_table_per_batch(norm, layout):
+    """Each batch at its own positions: the queries and keys of a call per batch
+    with that batch's table."""
+    torch = torch_mod()
+    B, L, N, H, d, C, off = 3, 40, 96, 2, 64, 128, 24
+    g = torch.Generator().manual_seed(460)
+    r = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).bfloat16().cuda()
+    x, kv, wo = r(B, L, C), r(2, B, N, H, d), r(H * d, C, scale=0.1)
+    wq, wk, wv = (r(C, H * d, scale=C ** -0.5) for _ in range(3))
+    cos, sin = (torch.empty(B, L, d // 2, device="cuda") for _ in range(2))
+    for b in range(B):
+        xd.xdit_rope_table(torch.arange(L, device="cuda")[:, None] + 1000 * b + off, [d], cos[b], sin[b])
+    w = dict(wq=1 + r(d, scale=0.3), wk=1 + r(d, scale=0.3)) if norm != "none" else {}
+    new = lambda *s: torch.full(s, float("nan"), device="cuda", dtype=torch.bfloat16)
+    q, k, v, o = (new(B, L, H, d) for _ in range(4))
+    y = new(B, L, C)
+    got_kv = kv.clone()
+    xd.xdit_stage_step(x, wq, wk, wv, wo, got_kv, off, q, k, v, o, y, norm=norm, cos=cos, sin=sin, layout=layout,
+                       **{"norm_" + n: t for n, t in w.items()})
+    # the projections of the plain step, then batch by batch
+    q1, k1, v1, o1 = (new(B, L, H, d) for _ in range(4))
+    xd.xdit_stage_step(x, wq, wk, wv, wo, kv.clone(), off, q1, k1, v1, o1, new(B, L, C))
+    for b in range(B):
+        xd.xdit_qk_norm_rope(q1[b:b + 1], k1[b:b + 1], q1[b:b + 1], k1[b:b + 1], norm=norm, cos=cos[b], sin=sin[b], layout=layout, **w)
+    assert torch.equal(q, q1) and torch.equal(k, k1) and not torch.equal(q[0], q[1])
+    want_kv = kv.clone()
+    xd.xdit_patch_attn(q1, want_kv, off, L, k1, v1, o1)
+    assert torch.equal(o, o1) and torch.equal(got_kv, want_kv) and torch.isfinite(y).all()
+
+
 def test_refusals():
     torch = torch_mod()
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, device="cuda", dtype=dt)
