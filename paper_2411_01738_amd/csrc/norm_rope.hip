@@ -15,10 +15,10 @@
 //
 // What bounds it: memory.  Each head is read and written once; the tables are
 // read once per token and batch of heads.  bf16, where a large copy reaches 5.1
-// TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 23.3 us (4.5
+// TB/s: RMS norms and rotation of 4224 tokens, 24 + 24 heads of 128, 22.6 us (4.7
 // TB/s; a copy of as much 21); layer norms and rotation of 17550 tokens, 48 + 48
-// heads of 64, 80 us (5.5 TB/s), their gradients 128 us (5.1 TB/s), the rotation of
-// one such tensor 43 us (5.1 TB/s).
+// heads of 64, 78 us (5.5 TB/s), their gradients 127 us (5.1 TB/s), the rotation of
+// one such tensor 42 us (5.1 TB/s).  float32: 41, 162, 267 and 83 us.
 //
 // Work: a lane holds 2 V values of a head, both elements of each of its
 // pairs, so the rotation needs no other lane: the runs at V p and D / 2 + V p for
@@ -376,12 +376,16 @@ struct NrGrid {
 
 // Workgroups along the tokens, a token per wave at a time: forward as many as
 // there are (up to 2^31 threads: a launch holds fewer than 2^32); backward, where
-// each sums its weights' gradients, no more than run at once, with as many tokens
-// for each.  Measured, us, at one round / twice that / a workgroup per 4 tokens
-// (backward four times): norms of 4224 tokens, 24 + 24 heads of 128 24.9 / 25.9 /
-// 24.5; 2 x 4096, 16 + 16 of 72 15.8 / 15.3 / 16.4; 17550, 48 + 48 of 64 90 / 88 /
-// 81; gradients of the three 39.8 / 41.2 / 43.1, 32.3 / 29.7 / 31.3, 127 / 130 /
-// 136; rotation of 17550, 48 heads of 64 49 / 51 / 44.
+// each sums its weights' gradients, at most 512 in all with as many tokens for
+// each.  So many run at once where a run is 8 values (184 to 206 registers, two
+// waves per SIMD); of the forms whose runs are 4 values (114 to 156) 768 or 1024
+// would.  Measured, us, at 512 / 1024 / 2048 workgroups: gradients of 4224 tokens,
+// 24 + 24 heads of 128 37.8 / 38.9 / 40.5, with 72 dims of the half layout rotated
+// (runs of 4) 46.7 / 40.6 / 39.7; 2 x 4096, 16 + 16 of 72 30.7 / 28.5 / 30.4;
+// 17550, 48 + 48 of 64, layer norm 128 / 129 / 136; float32: the first 70.2 / 69.4 /
+// 68.4, the last 267 / 266 / 262.  At 1024 / 2048 / a workgroup per 4 tokens: norms
+// of the first 22.8 / 24.5 / 22.9, of 2 x 4096 16.5 / 17.8 / 17.9, of 17550 89 / 87 /
+// 78; rotation of 17550, 48 heads of 64 48 / 45 / 41.
 NrGrid nr_grid(int64_t rows, int heads0, int heads1, int G, bool bwd) {
     NrGrid r;
     r.nb0 = (heads0 + kBatch * G - 1) / (kBatch * G);
@@ -511,9 +515,11 @@ __device__ __forceinline__ void quarter_sincos(double f, int quarters, double* s
 // the workgroup, in quarter turns and 64 bits (an angle of 10^6 in float32 is off
 // by 0.06), then per row the products with the position, their whole quarter turns
 // taken off exactly.  Bound by stores and 64-bit arithmetic, 25 operations an
-// angle, and by the start of one round of workgroups: 131072 x 64 angles take 20 us
-// (67 MB at 3.3 TB/s; one column a thread 26; the library's sincospi took 27), 2^20
-// x 64 125 us (4.3 TB/s; 191), 32768 x 64 8.6 (9.8).
+// angle, and by the start of one round of workgroups: 131072 x 64 angles take 18 to
+// 20 us (68 MB at 3.4 to 3.7 TB/s; one column a thread 26; the library's sincospi
+// took 27), 2^20 x 64 124 us (4.4 TB/s; 191), 32768 x 64 8.2 (9.8).  The highest term
+// of each series, and the product with a magnitude of 1, are more than a float32
+// table needs.
 //
 // Frequencies are 2^(i rate): the rounding of an exponent of size e would be
 // one of e ln 2 / 2 steps in the frequency (up to 7 measured at dims of 72, theta
