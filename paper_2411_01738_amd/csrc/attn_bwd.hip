@@ -9,8 +9,11 @@
 //   dV_j  = sum_i P_ij g_i
 //   dK_j  = sum_i dS_ij q_i / sqrt(d),  dQ_i = sum_j dS_ij k_j / sqrt(d)
 // The probabilities are computed again from the scores; nothing of size
-// queries x keys is stored.  P and dS are rounded to bf16 as operands of the
-// matrix cores (half a step, 2^-8 relative, each; the sums are float32).
+// queries x keys is stored.  P and dS are rounded to bf16 because they are
+// operands of bf16 products (half a step, 2^-8 relative, each; the sums are
+// float32).  The roundings of a sum's terms are independent: the root mean square
+// error of a result is 0.0024 relative where its own rounding gives 0.0017
+// (measured).  float32 products, which would keep them, run at a ninth of the rate.
 //
 // What bounds it: the matrix cores (24 heads of 128, 4224 x 4224: 683 us, 1120
 // TFLOP/s over the seven products, where a large product of random values
@@ -691,22 +694,26 @@ hipError_t launch_sweeps(const BwdArgs& kv, const BwdArgs& q, hipStream_t s) {
 
 }  // namespace
 
-// A model of the launch in microseconds.  A workgroup takes 6 us (operands,
-// first tiles, results) plus, per block of 32 streamed rows, `unit` for each of
-// its products (4 for dK and dV, 3 for dQ) with another workgroup on its CU.
-// 512 workgroups run at once; where they are fewer, the longest decides, at 0.65
-// of its time if it has its CU to itself; more of them take their sum's share
-// and most of one of the shorter ones, which come last, or as long as the
-// longest.  Cut sweeps add the join: a launch, and partials written and read at
-// 2 TB/s.
+// Ranks the cuts of a call by a model of its launch, in units near a microsecond
+// but no times: of its own choice it gives 0.6 to 1.5 times what is measured.  A
+// workgroup takes 6 (operands, first tiles, results) plus, per block of 32 streamed
+// rows, `unit` for each of its products (4 for dK and dV, 3 for dQ) with another
+// workgroup on its CU.  512 workgroups run at once (float32 at d <= 72: up to 768,
+// counted as 512); where they are fewer, the longest decides, at 0.65 of its time
+// if it has its CU to itself; more of them take their sum's share and most of one
+// of the shorter ones, which come last, or as long as the longest.  Cut sweeps add
+// the join: a launch, and partials written and read at 2 TB/s.
 // Measured in one part, and in the best, us: 2 x 16 heads of 72, 1024 x 1024 47
-// (dQ in 2: 56); 24 heads of 128, 512 x 4224 114, dQ in 2 104; 2 x 24 heads of
-// 64, 333 x 4429 84; 24 heads of 64, 1 x 4429 53, dQ in 4 24; 24 heads of 128,
-// 4224 x 64 129, dK/dV in 8 45; 3 heads of 128, 4224 x 4224 125, dQ in 3 and
-// dK/dV in 2 104; one head of 64, 8000 x 8000 116, dQ in 4 and dK/dV in 4 67;
-// float32, 2 heads of 64, 256 x 64 25, dQ in 2 and dK/dV in 8 13.  Over 86 calls
-// timed with all parts, the model's choice takes 1.9 % more time than the best in
-// the mean, at worst 33 %.
+// (dQ in 2: 53); 24 heads of 128, 512 x 4224 112, dQ in 2 101; 2 x 24 heads of
+// 64, 333 x 4429 81; 24 heads of 64, 1 x 4429 54, dQ in 4 24; 24 heads of 128,
+// 4224 x 64 129, dK/dV in 8 45; 3 heads of 128, 4224 x 4224 127, dQ in 3 and
+// dK/dV in 2 101; one head of 64, 8000 x 8000 118, dQ in 4 and dK/dV in 4 65;
+// float32, 2 heads of 64, 256 x 64 25, dQ in 2 and dK/dV in 8 13.  (One state per
+// call and short runs; calls among others on states in turn take 43 and 83 for the
+// first and the third.)  Over 86 calls timed under all cuts the choice takes 2.0 %
+// more time than the best in the mean; farthest off are float32, 12 heads of
+// 128, 85 x 592 (dQ in 6 38, in 4 29) and then four calls by 8 to 11 %; one, 12
+// heads of 128, 1100 x 4000, takes 6 % more than uncut.
 BwdSplits bwd_splits(int64_t bh, int64_t Nq, int64_t Nk, int D, bool bf16) {
     BwdSplits best{1, 1, bf16 ? kRows : 64};
     const int tile = bf16 && D <= 96 ? 64 : 32;
