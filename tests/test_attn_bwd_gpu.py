@@ -126,6 +126,15 @@ def test_whole_sequences(dtype, B, H, nq, nk, d):
     _sampled(206, B, nq, nk, H, d, dtype, [(B - 1, 5)], dlse=False)
 
 
+@pytest.mark.parametrize("dtype,nq,nk,H,d", [("bf16", 261000, 4, 32, 128), ("bf16", 5, 261000, 32, 128), ("f32", 130000, 3, 32, 128),
+                                             ("f32", 2, 130000, 32, 128)])
+def test_the_largest_batch(dtype, nq, nk, H, d):
+    """One batch of a tensor up to the 2 GiB that a call takes."""
+    es = 2 if dtype == "bf16" else 4
+    assert (1 << 31) - (1 << 24) < (max(nq, nk) + 256) * H * d * es < 1 << 31
+    _sampled(207, 1, nq, nk, H, d, dtype, [(0, 0), (0, H - 1)], dlse=True)
+
+
 @pytest.mark.parametrize("d", [64, 72, 128])
 def test_many_heads(d):
     _run(210, 2, 150, 170, 17, d, "bf16")

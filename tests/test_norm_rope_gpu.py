@@ -425,6 +425,86 @@ def test_weights_at_any_place(layout, rot):
                 assert torch.equal(a, c)
 
 
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("dtype,d,layout", [("bf16", 64, "interleaved"), ("bf16", 72, "half"), ("f32", 128, "interleaved")])
+def test_gradients_in_place(dtype, d, layout, norm):
+    """On q and k themselves, and on the gradients, all of them views of one
+    projection's rows: the bits of a call on dense tensors, nothing else written."""
+    torch = torch_mod()
+    r = Draws(45)
+    B, N, H, Hk, rot = 2, 37, 6, 3, 32
+    qkv, dqkv = r(B, N, H + 2 * Hk, d, dtype=dtype, scale=1.5), r(B, N, H + 2 * Hk, d, dtype=dtype)
+    w = dict(wq=r(d, dtype="f32", shift=1.0), wk=r(d, dtype="f32", shift=1.0))
+    cos, sin = r.angles(N, rot // 2)
+    cut = lambda t: (t[:, :, :H], t[:, :, H:H + Hk])
+    names = ("dwq", "dwk", "dbq", "dbk") if norm == "layer" else ("dwq", "dwk")
+
+    def call(q, k, gq, gk, dq, dk):
+        grad = {n: torch.full((d,), float("nan"), device="cuda") for n in names}
+        ws = torch.full((xd.qk_norm_rope_bwd_workspace_bytes(q, k) // 4,), float("nan"), device="cuda")
+        xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, dq, dk, norm=norm, cos=cos, sin=sin, layout=layout, workspace=ws, **w, **grad)
+        return list(grad.values())
+
+    dense = [t.contiguous() for t in (*cut(qkv), *cut(dqkv))]
+    want = [torch.empty_like(dense[0]), torch.empty_like(dense[1])]
+    sums = call(*dense, *want)
+    for on_inputs in (True, False):
+        x, g = qkv.clone(), dqkv.clone()
+        got = cut(x if on_inputs else g)
+        kept = (g if on_inputs else x).clone()
+        for a, b in zip(call(*cut(x), *cut(g), *got), sums):
+            assert torch.equal(a, b)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(g if on_inputs else x, kept)
+        assert torch.equal((x if on_inputs else g)[:, :, H + Hk:], (qkv if on_inputs else dqkv)[:, :, H + Hk:])
+
+
+def test_broadcast_inputs():
+    """Inputs with strides of zero (one token, one head or one batch for all)."""
+    torch = torch_mod()
+    r = Draws(46)
+    B, N, H, d = 3, 20, 4, 64
+    w = r(d, dtype="f32")
+    cos, sin = r.angles(N, d // 2)
+    kw = dict(norm="rms", wq=w, wk=w, cos=cos, sin=sin)
+    for shape in ((1, N, H, d), (B, 1, H, d), (B, N, 1, d), (1, 1, 1, d)):
+        q, g = (r(*shape).expand(B, N, H, d) for _ in range(2))
+        outs = []
+        for x, h in ((q, g), (q.contiguous(), g.contiguous())):
+            y = [torch.empty(B, N, H, d, device="cuda", dtype=torch.bfloat16) for _ in range(5)]
+            dw, ws = torch.empty(d, device="cuda"), torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(x, x), device="cuda", dtype=torch.uint8)
+            xd.xdit_qk_norm_rope(x, x, y[0], y[1], **kw)
+            xd.xdit_qk_norm_rope_bwd(x, x, h, h, y[2], y[3], **kw, dwk=dw, workspace=ws)
+            xd.xdit_rope(x, cos, sin, y[4], transpose=True)
+            outs.append((*y, dw))
+        for a, b in zip(*outs):
+            assert torch.equal(a, b), shape
+
+
+def test_some_of_the_weights():
+    """A weight or a bias of one side alone, and gradients of some of them: as
+    with ones and zeros in the others' place."""
+    torch = torch_mod()
+    r = Draws(47)
+    for d in (64, 72):
+        q, k, gq, gk = r(2, 21, 5, d), r(2, 21, 3, d), r(2, 21, 5, d), r(2, 21, 3, d)
+        cos, sin = r.angles(21, 12)
+        ones, zeros = torch.ones(d, device="cuda"), torch.zeros(d, device="cuda")
+        full = dict(wq=r(d, dtype="f32", shift=1.0), wk=r(d, dtype="f32", shift=1.0), bq=r(d, dtype="f32"), bk=r(d, dtype="f32"))
+        kw = dict(norm="layer", cos=cos, sin=sin)
+        ws = torch.empty(xd.qk_norm_rope_bwd_workspace_bytes(q, k), device="cuda", dtype=torch.uint8)
+        for some in (("wq",), ("wk",), ("bq",), ("bk",), ("wq", "bk"), ("wk", "bq")):
+            outs = []
+            for w in ({n: full[n] for n in some}, {n: full[n] if n in some else ones if n[0] == "w" else zeros for n in full}):
+                y = [torch.empty_like(t) for t in (q, k, q, k)]
+                grad = {"d" + n: torch.full((d,), float("nan"), device="cuda") for n in some}
+                xd.xdit_qk_norm_rope(q, k, y[0], y[1], **kw, **w)
+                xd.xdit_qk_norm_rope_bwd(q, k, gq, gk, y[2], y[3], **kw, **{n: t for n, t in w.items() if n[0] == "w"}, **grad, workspace=ws)
+                outs.append((*y, *grad.values()))
+            for a, b in zip(*outs):
+                assert torch.equal(a, b), some
+
+
 def test_no_query_heads():
     """Keys alone, beside queries of no heads."""
     torch = torch_mod()

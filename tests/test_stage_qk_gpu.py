@@ -102,6 +102,47 @@ def test_a_table_per_batch(norm, layout):
     assert torch.equal(o, o1) and torch.equal(got_kv, want_kv) and torch.isfinite(y).all()
 
 
+def test_stream_and_graph():
+    """On a stream of its own, and captured and replayed with other inputs: the
+    bits of the eager call."""
+    torch = torch_mod()
+    B, L, N, H, d, C, off = 2, 64, 160, 2, 72, 128, 48
+    g = torch.Generator().manual_seed(470)
+    r = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).bfloat16().cuda()
+    x, kv0, wo, w = r(B, L, C), r(2, B, N, H, d), r(H * d, C, scale=0.1), 1 + r(d, scale=0.3)
+    wq, wk, wv = (r(C, H * d, scale=C ** -0.5) for _ in range(3))
+    cos, sin = (torch.empty(L, d // 2, device="cuda") for _ in range(2))
+    xd.xdit_rope_table(torch.arange(L, device="cuda")[:, None] + off, [d], cos, sin)
+
+    def buffers():
+        return [kv0.clone(), *(torch.zeros(B, L, H, d, device="cuda", dtype=torch.bfloat16) for _ in range(4)),
+                torch.zeros(B, L, C, device="cuda", dtype=torch.bfloat16)]
+
+    def call(b):
+        xd.xdit_stage_step(x, wq, wk, wv, wo, b[0], off, *b[1:], norm="rms", norm_wq=w, norm_wk=w, cos=cos, sin=sin, layout="half")
+
+    eager, side, cap = buffers(), buffers(), buffers()
+    call(eager)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(side)
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(eager, side):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(cap)
+    for i in range(4):
+        x.copy_(r(B, L, C))
+        w.copy_(1 + r(d, scale=0.3))
+        graph.replay()
+        call(eager)
+        torch.cuda.synchronize()
+        for a, b in zip(eager, cap):
+            assert torch.equal(a, b), f"replay {i}"
+
+
 def test_refusals():
     torch = torch_mod()
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, device="cuda", dtype=dt)
